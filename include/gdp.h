@@ -481,6 +481,168 @@ typedef struct gdp_adam_tensor {
 int gdp_adam_step(int32_t n_tensors, const gdp_adam_tensor* tensors, int32_t dtype, float lr, float beta1,
                   float beta2, float eps, int64_t step, void* stream);
 
+/* ---- layer operators --------------------------------------------------------
+ *
+ * The parts of a placement layer (Section 3.2) as calls of their own, forward and
+ * backward, for layers of another make than gdp_placer_layer's: any width,
+ * attention with a learned relative position bias, causal order, key heads
+ * shared by query heads, queries for the last ops of a graph only.  X' = LN(X +
+ * MHA(X)), LN(Z + W_2 ReLU(W_1 Z + b_1) + b_2) are two calls a sublayer.
+ *
+ * All take row-major matrices with a row stride (ld, in elements, at least the
+ * row's width), element-aligned pointers of any alignment beyond that, and
+ * GDP_F32 or GDP_BF16 for every array but those named fp32.  Arithmetic is fp32
+ * or better; a bf16 result is rounded once (attention rounds probabilities and
+ * their gradients to bf16 as operands of the next product too).  Results do not
+ * depend on other work on the device: fixed summation orders, no atomics.
+ * Nothing is allocated, no memory is cleared by the runtime, and no call
+ * synchronises: all may be captured into a HIP graph.  An output may not overlap an
+ * input unless the call says so.  A row count of 0 is valid: nothing is written but
+ * the weights' gradients, which are then zero.
+ */
+#define GDP_MAX_NORM_WIDTH 8192   /* LayerNorm's row width                     */
+#define GDP_MAX_REL_BOUNDS 63     /* bucket bounds of the relative positions   */
+#define GDP_MAX_REL_LEN (1 << 28) /* positions of one graph                    */
+
+/*
+ * LayerNorm of a sum, as after a sublayer:
+ *   h = x + residual,  y = (h - mean) / sqrt(var + eps) gamma + beta,
+ * mean and (biased) variance over the row's width columns.
+ *   x         device [rows, width]
+ *   residual  device [rows, width], or NULL (then h = x)
+ *   gamma, beta  device [width]
+ *   y         device [rows, width] (output; may be x or residual)
+ *   sum       device [rows, width] (output, may be NULL; may be x or residual):
+ *             h, rounded to dtype: gdp_layer_norm_backward's h
+ * rows >= 0, 1 <= width <= GDP_MAX_NORM_WIDTH, eps >= 0.  No workspace.
+ */
+int gdp_layer_norm(int64_t rows, int32_t width, int32_t dtype, const void* x, int64_t ld_x, const void* residual,
+                   int64_t ld_res, const void* gamma, const void* beta, float eps, void* y, int64_t ld_y, void* sum,
+                   int64_t ld_sum, void* stream);
+
+/*
+ * Its gradients at h, with xhat = (h - mean) / sqrt(var + eps) formed again from h:
+ *   dh     = rstd (g - mean(g) - xhat mean(g xhat)) + dsum,  g = dy gamma
+ *   dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
+ *   h      device [rows, width] (x, or the sum that the forward kept)
+ *   dy     device [rows, width]
+ *   dsum   device [rows, width], or NULL: the gradient that reaches h past the LayerNorm
+ *   dh     device [rows, width] (output: the gradient of x and of residual; may be dy, h or dsum)
+ *   dgamma, dbeta  device [width] fp32 (outputs)
+ * Workspace: gdp_layer_norm_workspace_bytes(rows, width) (0 on invalid arguments).
+ */
+size_t gdp_layer_norm_workspace_bytes(int64_t rows, int32_t width);
+int gdp_layer_norm_backward(int64_t rows, int32_t width, int32_t dtype, const void* h, int64_t ld_h,
+                            const void* gamma, float eps, const void* dy, int64_t ld_dy, const void* dsum,
+                            int64_t ld_dsum, void* dh, int64_t ld_dh, float* dgamma, float* dbeta, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+typedef enum gdp_act { GDP_ACT_NONE = 0, GDP_ACT_RELU = 1 } gdp_act;
+
+/* A fully connected layer's sizes and row strides (those of arrays not given are not read). */
+typedef struct gdp_fc_layer {
+  int64_t rows;       /* 0 .. INT32_MAX                                       */
+  int32_t in_dim;     /* K >= 1                                               */
+  int32_t out_dim;    /* N >= 1                                               */
+  int32_t dtype;      /* gdp_dtype                                            */
+  int32_t act;        /* gdp_act                                              */
+  int64_t ld_x, ld_y, ld_res, ld_act, ld_dy, ld_dx, ld_dx_add;
+} gdp_fc_layer;
+
+/*
+ * a = act(x W^T + b),  y = a + residual.
+ *   x         device [rows, K]          w  device [N, K], contiguous
+ *   b         device [N], or NULL       residual  device [rows, N], or NULL
+ *   y         device [rows, N] (output; may be residual)
+ *   act_out   device [rows, N] (output, may be NULL): a, for the backward of a layer
+ *             with an activation and a residual (without residual y is a)
+ * No workspace.
+ */
+int gdp_fc(const gdp_fc_layer* f, const void* x, const void* w, const void* b, const void* residual, void* y,
+           void* act_out, void* stream);
+
+/*
+ * Its gradients, with dP = dy where a > 0 (ReLU) or dy:
+ *   dx = dP W + dx_add,  dw = dP^T x,  db = sum_rows dP      (residual's gradient is dy)
+ *   dy        device [rows, N]
+ *   act_out   device [rows, N]: a (read with GDP_ACT_RELU, else may be NULL)
+ *   dx_add    device [rows, K], or NULL: what reaches x on another path
+ *   dx        device [rows, K] (output, may be NULL; may be dx_add)
+ *   dw, db    device [N, K], [N] fp32 (outputs, each may be NULL)
+ * Workspace: gdp_fc_workspace_bytes(f) (0 on invalid arguments).
+ */
+size_t gdp_fc_workspace_bytes(const gdp_fc_layer* f);
+int gdp_fc_backward(const gdp_fc_layer* f, const void* dy, const void* x, const void* w, const void* act_out,
+                    const void* dx_add, void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
+ * Segment attention (Section 3.2) with a learned relative position bias by buckets.
+ * Graph g's keys and values are rows [key_start_h[g], + len_h[g]) of k and v, its
+ * positions 0 .. len - 1; its queries are its last n_query_h[g] positions, graph
+ * after graph in the rows of q (n_query_h NULL: every position; 1: one op
+ * appended to a graph whose keys and values are kept).  With S = seg_len and
+ * s0 = floor(p / S) S, the query at position p sees the keys j of
+ * [max(0, s0 - mem_len), min(s0 + S, len)), only j <= p if causal, whose key_mask
+ * byte is not 0:
+ *   z_j = scale q . k_j + table[h][bucket(j - p)],  o = sum_j softmax(z)_j v_j
+ * A query that sees no key gives zeros (lse -inf, gradients 0).  With
+ * f(d) = the number of bounds_h at or below d,
+ *   bucket(r) = f(|r|)                                     causal
+ *   bucket(r) = f(|r|), plus n_bounds + 1 where r > 0      else
+ * so that table is [n_heads, n_bounds + 1] or [n_heads, 2 n_bounds + 2].  Key head
+ * h / (n_heads / n_kv_heads) serves query head h; heads are contiguous column
+ * groups of head_dim.  A table entry below -1e30 excludes its bucket; others are
+ * at most 1e30 in magnitude.  What lies in rows that a query does not see,
+ * infinities and NaN included, does not reach its results.
+ */
+typedef struct gdp_rel_attn {
+  int32_t n_graphs;            /* 1 .. GDP_MAX_GRAPHS                         */
+  const int32_t* key_start_h;  /* host [G] >= 0                               */
+  const int32_t* len_h;        /* host [G], 0 .. GDP_MAX_REL_LEN              */
+  const int32_t* n_query_h;    /* host [G], 0 .. len_h[g], or NULL: len_h     */
+  int32_t n_heads;             /* >= 1                                        */
+  int32_t n_kv_heads;          /* divides n_heads                             */
+  int32_t head_dim;            /* 16, 32 or 64                                */
+  int32_t seg_len;             /* S >= 1                                      */
+  int32_t mem_len;             /* >= 0                                        */
+  int32_t causal;              /* 0 or 1                                      */
+  int32_t n_bounds;            /* 0 .. GDP_MAX_REL_BOUNDS                     */
+  const int32_t* bounds_h;     /* host [n_bounds], ascending, >= 1            */
+  int32_t dtype;               /* gdp_dtype                                   */
+  float scale;                 /* e.g. 1 / sqrt(head_dim)                     */
+  int64_t ld_q, ld_k, ld_v, ld_o;        /* row strides                       */
+  int64_t ld_do, ld_dq, ld_dk, ld_dv;    /* backward                          */
+} gdp_rel_attn;
+
+/* Workspace of gdp_rel_attention, or with backward = 1 of gdp_rel_attention_backward; 256 at
+ * least, 0 on invalid arguments (then gdp_last_error). */
+size_t gdp_rel_attention_workspace_bytes(const gdp_rel_attn* a, int32_t backward);
+
+/*
+ *   q  device [sum of queries, n_heads head_dim]     k, v  device [rows, n_kv_heads head_dim]
+ *   table     device [n_heads, buckets], contiguous
+ *   key_mask  device [rows] uint8, or NULL: every key
+ *   o         device [sum of queries, n_heads head_dim] (output)
+ *   lse       device [sum of queries, n_heads] fp32 (output, may be NULL): the base-2
+ *             logarithm of sum_j 2^(z_j log2 e), for the backward
+ */
+int gdp_rel_attention(const gdp_rel_attn* a, const void* q, const void* k, const void* v, const void* table,
+                      const uint8_t* key_mask, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/*
+ * Gradients for dL/do, from the forward's inputs, o and lse:
+ *   dq  device like q    dk, dv  device like k, v: every row of a graph's keys is written
+ *   (shared heads added up), other rows are left as they were
+ *   dtable  device [n_heads, buckets] fp32
+ * (outputs).  The graphs' key rows may not overlap.
+ */
+int gdp_rel_attention_backward(const gdp_rel_attn* a, const void* dout, const void* q, const void* k, const void* v,
+                               const void* table, const uint8_t* key_mask, const void* o, const float* lse, void* dq,
+                               void* dk, void* dv, float* dtable, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
 /*
  * Host-side check of a graph batch (all pointers host memory): graph_ptr
  * strictly increasing from 0, row_ptr monotone from 0 to E, col_idx in range,
@@ -554,6 +716,12 @@ typedef enum gdp_kernel_kind {
   GDP_K_LOGPROB,         /* log-probabilities of given placements           */
   GDP_K_GEMM_UPDATE_POOL, /* Eq. 3's update fused with the next layer's
                              Eq. 2 transform of the same rows               */
+  GDP_K_LAYER_NORM,      /* gdp_layer_norm                                    */
+  GDP_K_LAYER_NORM_BWD,  /* gdp_layer_norm_backward                           */
+  GDP_K_FC,              /* gdp_fc                                            */
+  GDP_K_FC_BWD,          /* gdp_fc_backward                                   */
+  GDP_K_REL_ATTENTION,   /* gdp_rel_attention                                 */
+  GDP_K_REL_ATTENTION_BWD, /* gdp_rel_attention_backward                      */
   GDP_K_COUNT
 } gdp_kernel_kind;
 

@@ -26,10 +26,11 @@ DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-p
 # to its MFMA accumulators on every tile: keeping them in ordinary VGPRs
 # avoids a copy to and from the accumulation registers around each use.
 FILE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-pass-failed"],
-              "train_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+              "train_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              "rel_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-Wno-pass-failed"]}
 
 SOURCES = ["graph_kernels.hip", "gemm.hip", "layer.hip", "attention.hip", "placer_kernels.hip", "sample.hip", "ppo.hip", "evaluate.hip", "evaluate_lanes.hip", "train.hip", "train_gemm.hip", "train_attn.hip",
-           "gdp_api.hip", "host_plan.cpp"]
+           "norm.hip", "fc.hip", "rel_attention.hip", "gdp_api.hip", "host_plan.cpp"]
 
 
 def _compile(src: str) -> str:

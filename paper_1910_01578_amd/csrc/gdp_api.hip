@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
@@ -11,6 +12,7 @@
 #include "gdp.h"
 #include "host_plan.h"
 #include "kernels.h"
+#include "op_kernels.h"
 #include "train_kernels.h"
 
 namespace gdp {
@@ -1382,6 +1384,237 @@ extern "C" int gdp_set_place_streams(int32_t n) {
   return GDP_OK;
 }
 
+// ---------------------------------------------------------------------------
+// Layer operators.
+// ---------------------------------------------------------------------------
+static bool element_aligned(const void* p, int32_t dtype) { return ((uintptr_t)p & (elem_size(dtype) - 1)) == 0; }
+
+// Every array of a call: NULL is an error unless it is optional.
+struct OpArray {
+  const char* name;
+  const void* p;
+  bool optional;
+  int32_t dtype;
+};
+static int check_arrays(std::initializer_list<OpArray> arrays) {
+  for (const OpArray& a : arrays) {
+    if (!a.p && !a.optional) return fail(GDP_E_INVALID_ARG, "%s is NULL", a.name);
+    if (!element_aligned(a.p, a.dtype)) return fail(GDP_E_INVALID_ARG, "%s is not aligned to its elements", a.name);
+  }
+  return GDP_OK;
+}
+
+extern "C" int gdp_layer_norm(int64_t rows, int32_t width, int32_t dtype, const void* x, int64_t ld_x,
+                              const void* residual, int64_t ld_res, const void* gamma, const void* beta, float eps,
+                              void* y, int64_t ld_y, void* sum, int64_t ld_sum, void* stream) {
+  clear_error();
+  int r = check_norm(rows, width, dtype, eps);
+  if (r == GDP_OK && rows == 0) return GDP_OK;
+  if (r == GDP_OK)
+    r = check_arrays({{"x", x, false, dtype}, {"residual", residual, true, dtype}, {"gamma", gamma, false, dtype},
+                      {"beta", beta, false, dtype}, {"y", y, false, dtype}, {"sum", sum, true, dtype}});
+  if (r == GDP_OK) r = check_ld("ld_x", ld_x, width);
+  if (r == GDP_OK && residual) r = check_ld("ld_res", ld_res, width);
+  if (r == GDP_OK) r = check_ld("ld_y", ld_y, width);
+  if (r == GDP_OK && sum) r = check_ld("ld_sum", ld_sum, width);
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    op::NormArgs<T> a = {};
+    a.rows = rows;
+    a.width = width;
+    a.x = static_cast<const T*>(x);
+    a.ldx = ld_x;
+    a.res = static_cast<const T*>(residual);
+    a.ldr = ld_res;
+    a.gamma = static_cast<const T*>(gamma);
+    a.beta = static_cast<const T*>(beta);
+    a.eps = eps;
+    a.y = static_cast<T*>(y);
+    a.ldy = ld_y;
+    a.sum = static_cast<T*>(sum);
+    a.lds = ld_sum;
+    GDP_LAUNCH(GDP_K_LAYER_NORM, op::launch_norm<T>(a, st));
+    return GDP_OK;
+  };
+  return dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
+extern "C" size_t gdp_layer_norm_workspace_bytes(int64_t rows, int32_t width) {
+  clear_error();
+  if (check_norm(rows, width, GDP_F32, 0.f) != GDP_OK) return 0;
+  return ((size_t)norm_backward_blocks(rows, width) * 2 * width * 4 + 255) / 256 * 256 + 256;
+}
+
+extern "C" int gdp_layer_norm_backward(int64_t rows, int32_t width, int32_t dtype, const void* h, int64_t ld_h,
+                                       const void* gamma, float eps, const void* dy, int64_t ld_dy, const void* dsum,
+                                       int64_t ld_dsum, void* dh, int64_t ld_dh, float* dgamma, float* dbeta,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  int r = check_norm(rows, width, dtype, eps);
+  const bool any = rows > 0;
+  if (r == GDP_OK)
+    r = check_arrays({{"h", h, !any, dtype}, {"gamma", gamma, !any, dtype}, {"dy", dy, !any, dtype},
+                      {"dsum", dsum, true, dtype}, {"dh", dh, !any, dtype}, {"dgamma", dgamma, false, GDP_F32},
+                      {"dbeta", dbeta, false, GDP_F32}});
+  if (r == GDP_OK && any) r = check_ld("ld_h", ld_h, width);
+  if (r == GDP_OK && any) r = check_ld("ld_dy", ld_dy, width);
+  if (r == GDP_OK && any && dsum) r = check_ld("ld_dsum", ld_dsum, width);
+  if (r == GDP_OK && any) r = check_ld("ld_dh", ld_dh, width);
+  if (r == GDP_OK) r = check_ws(workspace, workspace_bytes, (size_t)norm_backward_blocks(rows, width) * 2 * width * 4);
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    op::NormArgs<T> a = {};
+    a.rows = rows;
+    a.width = width;
+    a.x = static_cast<const T*>(h);
+    a.ldx = ld_h;
+    a.res = static_cast<const T*>(dsum);
+    a.ldr = ld_dsum;
+    a.gamma = static_cast<const T*>(gamma);
+    a.eps = eps;
+    a.dy = static_cast<const T*>(dy);
+    a.lddy = ld_dy;
+    a.y = static_cast<T*>(dh);
+    a.ldy = ld_dh;
+    GDP_LAUNCH(GDP_K_LAYER_NORM_BWD, op::launch_norm_backward<T>(a, static_cast<float*>(workspace), dgamma, dbeta, st));
+    return GDP_OK;
+  };
+  return dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
+extern "C" int gdp_fc(const gdp_fc_layer* f, const void* x, const void* w, const void* b, const void* residual, void* y,
+                      void* act_out, void* stream) {
+  clear_error();
+  int r = check_fc(f);
+  if (r != GDP_OK || f->rows == 0) return r;
+  r = check_arrays({{"x", x, false, f->dtype}, {"w", w, false, f->dtype}, {"b", b, true, f->dtype},
+                    {"residual", residual, true, f->dtype}, {"y", y, false, f->dtype}, {"act_out", act_out, true, f->dtype}});
+  if (r == GDP_OK) r = check_ld("ld_x", f->ld_x, f->in_dim);
+  if (r == GDP_OK) r = check_ld("ld_y", f->ld_y, f->out_dim);
+  if (r == GDP_OK && residual) r = check_ld("ld_res", f->ld_res, f->out_dim);
+  if (r == GDP_OK && act_out) r = check_ld("ld_act", f->ld_act, f->out_dim);
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    GDP_LAUNCH(GDP_K_FC, op::launch_fc<T>(*f, static_cast<const T*>(x), static_cast<const T*>(w), static_cast<const T*>(b),
+                                          static_cast<const T*>(residual), static_cast<T*>(y), static_cast<T*>(act_out), st));
+    return GDP_OK;
+  };
+  return f->dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
+extern "C" size_t gdp_fc_workspace_bytes(const gdp_fc_layer* f) {
+  clear_error();
+  if (check_fc(f) != GDP_OK) return 0;
+  FcPlan p;
+  plan_fc_backward(f, &p);
+  return p.c.total;
+}
+
+extern "C" int gdp_fc_backward(const gdp_fc_layer* f, const void* dy, const void* x, const void* w, const void* act_out,
+                               const void* dx_add, void* dx, float* dw, float* db, void* workspace, size_t workspace_bytes, void* stream) {
+  clear_error();
+  int r = check_fc(f);
+  if (r != GDP_OK) return r;
+  const bool any = f->rows > 0, relu = f->act == GDP_ACT_RELU;
+  r = check_arrays({{"dy", dy, !any, f->dtype}, {"x", x, !any, f->dtype}, {"w", w, !any, f->dtype},
+                    {"act_out", act_out, !any || !relu, f->dtype}, {"dx_add", dx_add, true, f->dtype}, {"dx", dx, true, f->dtype}, {"dw", dw, true, GDP_F32},
+                    {"db", db, true, GDP_F32}});
+  if (r == GDP_OK && any) r = check_ld("ld_dy", f->ld_dy, f->out_dim);
+  if (r == GDP_OK && any) r = check_ld("ld_x", f->ld_x, f->in_dim);
+  if (r == GDP_OK && any && relu) r = check_ld("ld_act", f->ld_act, f->out_dim);
+  if (r == GDP_OK && any && dx) r = check_ld("ld_dx", f->ld_dx, f->in_dim);
+  if (r == GDP_OK && any && dx_add) r = check_ld("ld_dx_add", f->ld_dx_add, f->in_dim);
+  FcPlan p;
+  if (r == GDP_OK) {
+    plan_fc_backward(f, &p);
+    r = check_ws(workspace, workspace_bytes, p.c.total);
+  }
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    GDP_LAUNCH(GDP_K_FC_BWD, op::launch_fc_backward<T>(*f, p, static_cast<const T*>(dy), static_cast<const T*>(x),
+                                                       static_cast<const T*>(w), static_cast<const T*>(act_out),
+                                                       static_cast<const T*>(dx_add), static_cast<T*>(dx), dw, db, workspace, st));
+    return GDP_OK;
+  };
+  return f->dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
+extern "C" size_t gdp_rel_attention_workspace_bytes(const gdp_rel_attn* a, int32_t backward) {
+  clear_error();
+  if (backward != 0 && backward != 1) return fail(GDP_E_INVALID_ARG, "backward = %d must be 0 or 1", backward), 0;
+  if (check_rel(a, backward != 0) != GDP_OK) return 0;
+  RelPlan p;
+  plan_rel(a, backward != 0, &p);
+  return p.c.total;
+}
+
+extern "C" int gdp_rel_attention(const gdp_rel_attn* a, const void* q, const void* k, const void* v, const void* table,
+                                 const uint8_t* key_mask, void* o, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  clear_error();
+  int r = check_rel(a, false);
+  if (r != GDP_OK) return r;
+  RelPlan p;
+  plan_rel(a, false, &p);
+  if (p.queries == 0) return GDP_OK;
+  r = check_arrays({{"q", q, false, a->dtype}, {"k", k, false, a->dtype}, {"v", v, false, a->dtype},
+                    {"table", table, false, a->dtype}, {"o", o, false, a->dtype}, {"lse", lse, true, GDP_F32}});
+  if (r == GDP_OK) r = check_ws(workspace, workspace_bytes, p.c.total);
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    GDP_LAUNCH(GDP_K_REL_ATTENTION,
+               op::launch_rel_attention<T>(*a, p, static_cast<const T*>(q), static_cast<const T*>(k), static_cast<const T*>(v),
+                                           static_cast<const T*>(table), key_mask, static_cast<T*>(o), lse, workspace, st));
+    return GDP_OK;
+  };
+  return a->dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
+extern "C" int gdp_rel_attention_backward(const gdp_rel_attn* a, const void* dout, const void* q, const void* k,
+                                          const void* v, const void* table, const uint8_t* key_mask, const void* o,
+                                          const float* lse, void* dq, void* dk, void* dv, float* dtable, void* workspace,
+                                          size_t workspace_bytes, void* stream) {
+  clear_error();
+  int r = check_rel(a, true);
+  if (r != GDP_OK) return r;
+  RelPlan p;
+  plan_rel(a, true, &p);
+  const bool nq = p.queries == 0, nk = p.key_blocks == 0;
+  r = check_arrays({{"dout", dout, nq, a->dtype}, {"q", q, nq, a->dtype}, {"k", k, nk, a->dtype}, {"v", v, nk, a->dtype},
+                    {"table", table, nk, a->dtype}, {"o", o, nq, a->dtype}, {"lse", lse, nq, GDP_F32}, {"dq", dq, nq, a->dtype},
+                    {"dk", dk, nk, a->dtype}, {"dv", dv, nk, a->dtype}, {"dtable", dtable, false, GDP_F32}});
+  if (r == GDP_OK) r = check_ws(workspace, workspace_bytes, p.c.total);
+  if (r == GDP_OK) r = pending_hip_error();
+  if (r != GDP_OK) return r;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  auto run = [&](auto t) -> int {
+    using T = decltype(t);
+    GDP_LAUNCH(GDP_K_REL_ATTENTION_BWD,
+               op::launch_rel_attention_backward<T>(*a, p, static_cast<const T*>(dout), static_cast<const T*>(q),
+                                                    static_cast<const T*>(k), static_cast<const T*>(v),
+                                                    static_cast<const T*>(table), key_mask, static_cast<const T*>(o), lse,
+                                                    static_cast<T*>(dq), static_cast<T*>(dk), static_cast<T*>(dv), dtable,
+                                                    workspace, st));
+    return GDP_OK;
+  };
+  return a->dtype == GDP_BF16 ? run(bf16()) : run(float());
+}
+
 extern "C" int gdp_timer_begin(uint32_t mask) {
   clear_error();
   if (g_timer.mask != 0 || !g_timer.recs.empty()) return fail(GDP_E_INVALID_ARG, "timer already running");
@@ -1421,7 +1654,8 @@ extern "C" const char* gdp_kernel_kind_name(int32_t kind) {
       "graph_prep", "nbr_sample",    "gemm_pool_sigmoid", "gather_max", "gemm_update_relu",
       "meanpool",   "film",          "pre_layer",         "seg_attention", "post_attn",
       "head_lse",   "gumbel_sample", "logp_reduce",       "mlp_placer", "ppo_grad",  "head_backward", "advantages",
-      "evaluate", "train_forward", "backward", "adam", "log_prob", "gemm_update_pool"};
+      "evaluate", "train_forward", "backward", "adam", "log_prob", "gemm_update_pool", "layer_norm",
+      "layer_norm_backward", "fc", "fc_backward", "rel_attention", "rel_attention_backward"};
   if (kind < 0 || kind >= GDP_K_COUNT) return "";
   return names[kind];
 }

@@ -1,11 +1,13 @@
 // Host-only argument checks, workspace planning and the graph validator.
 #include "host_plan.h"
 
+#include <float.h>
 #include <limits.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <vector>
 
 namespace gdp {
@@ -367,6 +369,171 @@ void plan_sample(const gdp_graph* g, int32_t k, SamplePlan* p) {
   carve_init(&p->c);
   p->partial = carve_add(&p->c, (size_t)k * p->chunks * 4);
   p->coef = carve_add(&p->c, (size_t)g->n_graphs * (k + 1) * 4);
+}
+
+// ---------------------------------------------------------------------------
+// Layer operators.
+// ---------------------------------------------------------------------------
+int norm_backward_blocks(int64_t rows, int32_t width) {
+  const int64_t most = std::max<int64_t>(256, (1 << 20) / width);
+  return (int)std::min<int64_t>(std::min<int64_t>(1024, most), std::min<int64_t>(rows, (rows * width + 4095) / 4096));
+}
+
+static int check_dtype(int32_t dtype) {
+  if (dtype != GDP_F32 && dtype != GDP_BF16) return fail(GDP_E_INVALID_ARG, "dtype = %d", dtype);
+  return GDP_OK;
+}
+
+int check_norm(int64_t rows, int32_t width, int32_t dtype, float eps) {
+  if (rows < 0) return fail(GDP_E_INVALID_ARG, "rows = %lld < 0", (long long)rows);
+  if (rows > INT64_MAX / 65536) return fail(GDP_E_UNSUPPORTED, "rows = %lld", (long long)rows);
+  if (width < 1) return fail(GDP_E_INVALID_ARG, "width = %d < 1", width);
+  if (width > GDP_MAX_NORM_WIDTH)
+    return fail(GDP_E_UNSUPPORTED, "width = %d exceeds GDP_MAX_NORM_WIDTH = %d", width, GDP_MAX_NORM_WIDTH);
+  if (!(eps >= 0.f) || eps > FLT_MAX) return fail(GDP_E_INVALID_ARG, "eps = %g must be finite and >= 0", (double)eps);
+  return check_dtype(dtype);
+}
+
+int check_ld(const char* name, int64_t ld, int64_t least) {
+  if (ld < least) return fail(GDP_E_INVALID_ARG, "%s = %lld < %lld", name, (long long)ld, (long long)least);
+  if (ld > (int64_t(1) << 40)) return fail(GDP_E_UNSUPPORTED, "%s = %lld", name, (long long)ld);
+  return GDP_OK;
+}
+
+int check_fc(const gdp_fc_layer* f) {
+  if (!f) return fail(GDP_E_INVALID_ARG, "fc layer is NULL");
+  if (f->rows < 0) return fail(GDP_E_INVALID_ARG, "rows = %lld < 0", (long long)f->rows);
+  if (f->in_dim < 1 || f->out_dim < 1)
+    return fail(GDP_E_INVALID_ARG, "in_dim = %d and out_dim = %d must be at least 1", f->in_dim, f->out_dim);
+  if (f->act != GDP_ACT_NONE && f->act != GDP_ACT_RELU) return fail(GDP_E_INVALID_ARG, "act = %d", f->act);
+  if (f->rows > INT32_MAX) return fail(GDP_E_UNSUPPORTED, "rows = %lld exceeds %d", (long long)f->rows, INT32_MAX);
+  // tiles of 64 x 64 at the least
+  const int64_t m = f->rows / 64 + 1, k = f->in_dim / 64 + 1, n = f->out_dim / 64 + 1;
+  if (m * std::max(k, n) > INT32_MAX / 64 || k * n > INT32_MAX / 64)
+    return fail(GDP_E_UNSUPPORTED, "%lld rows of %d to %d are too many tiles", (long long)f->rows, f->in_dim, f->out_dim);
+  return check_dtype(f->dtype);
+}
+
+void plan_fc_backward(const gdp_fc_layer* f, FcPlan* p) {
+  carve_init(&p->c);
+  const int64_t M = f->rows, K = f->in_dim, N = f->out_dim;
+  const bool f32 = f->dtype == GDP_F32;
+  const int64_t vec = f32 ? 4 : 8;
+  // ReLU's gradient is a selection of dy; and the fp32 products tell a matrix's order by
+  // which stride is 1, so a column (row stride 1) is copied too
+  p->ldp = f->act == GDP_ACT_RELU || (f32 && f->ld_dy == 1) ? (N + vec - 1) / vec * vec : 0;
+  p->dp = carve_add(&p->c, (size_t)(p->ldp * M) * elem_size(f->dtype));
+  if (f32) {
+    const int64_t pieces = std::min<int64_t>(64, std::max<int64_t>(1, M / 256));
+    p->partial_floats = (N * (K + 1) * pieces + 63) / 64 * 64;
+    p->splits = p->rows_per_split = 0;
+    p->partial = carve_add(&p->c, (size_t)(p->partial_floats + N * K) * 4);
+  } else {
+    // two work-groups per CU, each at least 256 rows of the sum
+    const int64_t tiles = ((N + 127) / 128) * ((K + 127) / 128);
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, (M + 255) / 256));
+    const int64_t per = std::max<int64_t>(64, ((M + want - 1) / want + 63) / 64 * 64);
+    p->rows_per_split = (int)std::min<int64_t>(per, INT32_MAX / 64 * 64);
+    p->splits = (int)std::max<int64_t>(1, (M + p->rows_per_split - 1) / p->rows_per_split);
+    p->partial_floats = 0;
+    p->partial = carve_add(&p->c, (size_t)p->splits * (size_t)(N * K + N) * 4);
+  }
+}
+
+static int rel_queries(const gdp_rel_attn* a, int g) { return a->n_query_h ? a->n_query_h[g] : a->len_h[g]; }
+
+int check_rel(const gdp_rel_attn* a, bool backward) {
+  if (!a) return fail(GDP_E_INVALID_ARG, "attention is NULL");
+  if (a->n_graphs < 1) return fail(GDP_E_INVALID_ARG, "n_graphs = %d < 1", a->n_graphs);
+  if (a->n_graphs > GDP_MAX_GRAPHS)
+    return fail(GDP_E_UNSUPPORTED, "n_graphs = %d exceeds GDP_MAX_GRAPHS = %d", a->n_graphs, GDP_MAX_GRAPHS);
+  if (!a->key_start_h || !a->len_h) return fail(GDP_E_INVALID_ARG, "key_start_h or len_h is NULL");
+  if (a->n_heads < 1 || a->n_kv_heads < 1 || a->n_heads % a->n_kv_heads != 0)
+    return fail(GDP_E_INVALID_ARG, "n_heads = %d is not a positive multiple of n_kv_heads = %d", a->n_heads, a->n_kv_heads);
+  if (a->head_dim != 16 && a->head_dim != 32 && a->head_dim != 64)
+    return fail(GDP_E_UNSUPPORTED, "head_dim = %d not in {16,32,64}", a->head_dim);
+  if (a->seg_len < 1) return fail(GDP_E_INVALID_ARG, "seg_len = %d < 1", a->seg_len);
+  if (a->mem_len < 0) return fail(GDP_E_INVALID_ARG, "mem_len = %d < 0", a->mem_len);
+  if (a->causal != 0 && a->causal != 1) return fail(GDP_E_INVALID_ARG, "causal = %d must be 0 or 1", a->causal);
+  if (a->n_bounds < 0) return fail(GDP_E_INVALID_ARG, "n_bounds = %d < 0", a->n_bounds);
+  if (a->n_bounds > GDP_MAX_REL_BOUNDS)
+    return fail(GDP_E_UNSUPPORTED, "n_bounds = %d exceeds GDP_MAX_REL_BOUNDS = %d", a->n_bounds, GDP_MAX_REL_BOUNDS);
+  if (a->n_bounds > 0 && !a->bounds_h) return fail(GDP_E_INVALID_ARG, "bounds_h is NULL");
+  for (int i = 0; i < a->n_bounds; ++i)
+    if (a->bounds_h[i] < 1 || (i > 0 && a->bounds_h[i] <= a->bounds_h[i - 1]))
+      return fail(GDP_E_INVALID_ARG, "bounds_h[%d] = %d: the bounds must ascend from 1 on", i, a->bounds_h[i]);
+  if (!(a->scale >= -FLT_MAX && a->scale <= FLT_MAX)) return fail(GDP_E_INVALID_ARG, "scale is not finite");
+  int r = check_dtype(a->dtype);
+  if (r != GDP_OK) return r;
+  int64_t queries = 0, qblocks = 0, kblocks = 0;
+  for (int g = 0; g < a->n_graphs; ++g) {
+    const int len = a->len_h[g];
+    if (len < 0 || a->key_start_h[g] < 0)
+      return fail(GDP_E_INVALID_ARG, "graph %d: key_start_h = %d and len_h = %d must not be negative", g, a->key_start_h[g], len);
+    if (len > GDP_MAX_REL_LEN) return fail(GDP_E_UNSUPPORTED, "len_h[%d] = %d exceeds GDP_MAX_REL_LEN", g, len);
+    const int nq = rel_queries(a, g);
+    if (nq < 0 || nq > len) return fail(GDP_E_INVALID_ARG, "n_query_h[%d] = %d outside 0..%d", g, nq, len);
+    queries += nq;
+    qblocks += (nq + 63) / 64;
+    kblocks += (len + 63) / 64;
+    if (backward)
+      for (int h = 0; h < g; ++h)
+        if (len > 0 && a->len_h[h] > 0 && a->key_start_h[g] < (int64_t)a->key_start_h[h] + a->len_h[h] &&
+            a->key_start_h[h] < (int64_t)a->key_start_h[g] + len)
+          return fail(GDP_E_INVALID_ARG, "the key rows of graphs %d and %d overlap", h, g);
+  }
+  if (queries > INT32_MAX || std::max(qblocks, kblocks) * a->n_heads > INT32_MAX / 64)
+    return fail(GDP_E_UNSUPPORTED, "%lld queries of %d heads are too many", (long long)queries, a->n_heads);
+  const int64_t wq = (int64_t)a->n_heads * a->head_dim, wk = (int64_t)a->n_kv_heads * a->head_dim;
+  r = check_ld("ld_q", a->ld_q, wq);
+  if (r == GDP_OK) r = check_ld("ld_k", a->ld_k, wk);
+  if (r == GDP_OK) r = check_ld("ld_v", a->ld_v, wk);
+  if (r == GDP_OK) r = check_ld("ld_o", a->ld_o, wq);
+  if (r == GDP_OK && backward) r = check_ld("ld_do", a->ld_do, wq);
+  if (r == GDP_OK && backward) r = check_ld("ld_dq", a->ld_dq, wq);
+  if (r == GDP_OK && backward) r = check_ld("ld_dk", a->ld_dk, wk);
+  if (r == GDP_OK && backward) r = check_ld("ld_dv", a->ld_dv, wk);
+  return r;
+}
+
+void plan_rel(const gdp_rel_attn* a, bool backward, RelPlan* p) {
+  carve_init(&p->c);
+  int longest = 1;
+  int64_t wide = 0, wide_keys = 0;                 // blocks of 128
+  p->queries = 0;
+  for (int g = 0; g < a->n_graphs; ++g) {
+    longest = std::max(longest, a->len_h[g]);
+    p->queries += rel_queries(a, g);
+    wide += (rel_queries(a, g) + 127) / 128;
+    wide_keys += (a->len_h[g] + 127) / 128;
+  }
+  p->seg = std::min(a->seg_len, longest);
+  p->mem = std::min(a->mem_len, longest);
+  p->buckets = (a->n_bounds + 1) * (a->causal ? 1 : 2);
+  // Two columns a wave halve the tile reads a product, where that leaves two work-groups
+  // a CU and the registers hold them (not three planes of d_h = 64, nor backward three
+  // planes or d_h = 64: they spill).
+  const bool fits = a->dtype == GDP_BF16 || a->head_dim < 64;
+  p->cols = fits && wide * a->n_heads >= 512 ? 2 : 1;
+  p->bwd_cols = a->dtype == GDP_BF16 && a->head_dim < 64 &&
+                        std::min(wide * a->n_heads, wide_keys * a->n_kv_heads) >= 512 ? 2 : 1;
+  // Few queries: about two work-groups a CU in all, each at least 4 tiles of 64 keys.
+  int most = 0;
+  int64_t groups = 0;
+  for (int g = 0; g < a->n_graphs; ++g) {
+    most = std::max(most, rel_queries(a, g));
+    groups += ((int64_t)rel_queries(a, g) * (a->n_heads / a->n_kv_heads) + 15) / 16 * a->n_kv_heads;
+  }
+  p->parts = 0;
+  const int64_t seen = std::min<int64_t>(longest, (int64_t)p->seg + p->mem + kRelFewQueries);
+  if (!backward && most > 0 && most <= kRelFewQueries)
+    p->parts = (int)std::max<int64_t>(1, std::min<int64_t>((512 + groups - 1) / groups, (seen + 255) / 256));
+  p->key_blocks = 0;
+  for (int g = 0; g < a->n_graphs; ++g) p->key_blocks += (a->len_h[g] + 64 * p->bwd_cols - 1) / (64 * p->bwd_cols);
+  p->d = carve_add(&p->c, backward ? (size_t)p->queries * a->n_heads * 4
+                          : p->parts > 1 ? (size_t)p->queries * a->n_heads * p->parts * (a->head_dim + 4) * 4 : 256);
+  p->table_partial = carve_add(&p->c, backward ? (size_t)p->key_blocks * a->n_heads * p->buckets * 4 : 0);
+  if (p->c.total == 0) carve_add(&p->c, 256);
 }
 
 }  // namespace gdp

@@ -120,6 +120,38 @@ void plan_embed(const gdp_graph* g, const gdp_gnn* gnn, EmbedPlan* p);
 void plan_place(const gdp_graph* g, const gdp_placer* pl, PlacePlan* p);
 void plan_sample(const gdp_graph* g, int32_t k_samples, SamplePlan* p);
 
+// ---- layer operators -----------------------------------------------------------
+// Row groups of LayerNorm's backward, each with one row of partial sums: enough to fill
+// the chip, of 4,096 elements at least, and their sums at most 2^20 floats a kind.
+int norm_backward_blocks(int64_t rows, int32_t width);
+int check_norm(int64_t rows, int32_t width, int32_t dtype, float eps);
+int check_ld(const char* name, int64_t ld, int64_t least);
+
+constexpr int kFcFewRows = 64;      // rows up to which a FC layer deals k to a work-group's waves
+int check_fc(const gdp_fc_layer* f);
+struct FcPlan {
+  Carve c;
+  size_t dp, partial;
+  int64_t ldp;             // row stride of dP's copy in the workspace, 0: dy is used as it is
+  int64_t partial_floats;  // fp32: the products' split sums
+  int splits, rows_per_split;  // bf16: dW's pieces of rows
+};
+void plan_fc_backward(const gdp_fc_layer* f, FcPlan* p);
+
+int check_rel(const gdp_rel_attn* a, bool backward);
+constexpr int kRelFewQueries = 64;  // queries a graph up to which the keys are split over work-groups
+struct RelPlan {
+  Carve c;
+  int seg, mem;            // less where longer ones make no difference
+  int buckets;
+  int cols, bwd_cols;      // 16-row columns a wave owns
+  int parts;               // forward with few queries: parts of the keys, each a work-group; else 0
+  int64_t queries;         // rows of q
+  int key_blocks;          // work-groups a head of the dK, dV kernel
+  size_t d, table_partial;
+};
+void plan_rel(const gdp_rel_attn* a, bool backward, RelPlan* p);
+
 constexpr int kPoolRows = 64;       // rows per mean-pool chunk
 constexpr int kAttnQ = 128;         // queries per attention work-group
 // Rows of part A of the two-part layer schedule: 256 blocks of 128 rows, one

@@ -158,11 +158,11 @@ struct Stage {
 };
 
 // The epilogue as a compile-time set of operations.
-enum Epi { E_RAW = 0, E_BIAS = 1, E_RELU = 2, E_SIGMOID = 4, E_MASK = 8, E_RES = 16, E_ACC = 32 };
+enum Epi { E_RAW = 0, E_BIAS = 1, E_RELU = 2, E_SIGMOID = 4, E_MASK = 8, E_RES = 16, E_ACC = 32, E_GATE = 64 };
 
 template <typename TA, typename TB>
 int epi_of(const GemmStrided<TA, TB>& g) {
-  return (g.bias_f || g.bias_h ? E_BIAS : 0) | (g.act == ACT_RELU ? E_RELU : g.act == ACT_SIGMOID ? E_SIGMOID : 0) |
+  return (g.bias_f || g.bias_h ? E_BIAS : 0) | (g.act == ACT_RELU ? E_RELU : g.act == ACT_SIGMOID ? E_SIGMOID : g.act == ACT_GATE ? E_GATE : 0) |
          (g.mask ? E_MASK : 0) | (g.res ? E_RES : 0) | (g.accumulate ? E_ACC : 0);
 }
 
@@ -196,6 +196,7 @@ __device__ __forceinline__ void epilogue(const GemmStrided<TA, TB>& g, int m, in
     if constexpr ((EPI & E_BIAS) != 0) v[r] += in.bias[r];
     if constexpr ((EPI & E_RELU) != 0) v[r] = fmaxf(v[r], 0.f);
     if constexpr ((EPI & E_SIGMOID) != 0) v[r] = sigmoidf_(v[r]);
+    if constexpr ((EPI & E_GATE) != 0) v[r] = v[r] < 0.f ? 0.f : v[r];
     if constexpr ((EPI & E_MASK) != 0) v[r] = in.mask.v[r] > 0.f ? v[r] : 0.f;
     if constexpr ((EPI & E_RES) != 0) v[r] += in.res.v[r];
     if constexpr ((EPI & E_ACC) != 0) v[r] += in.old.v[r];
@@ -703,6 +704,16 @@ hipError_t launch_gemm_strided(const GemmStrided<TA, TB>& g, float* partial, siz
         GDP_GEMM_CASE(E_BIAS | E_RELU, true, true);
         GDP_GEMM_CASE(E_BIAS | E_RES, true, true);
         GDP_GEMM_CASE(E_ACC, true, true);
+      }
+    }
+    if constexpr (std::is_same<TA, float>::value && std::is_same<TB, float>::value) {   // the layer operators' FC
+      switch (epi) {
+        GDP_GEMM_CASE(E_RAW, true, true);
+        GDP_GEMM_CASE(E_GATE, true, true);
+        GDP_GEMM_CASE(E_RES, true, true);
+        GDP_GEMM_CASE(E_GATE | E_RES, true, true);
+        GDP_GEMM_CASE(E_BIAS | E_GATE, true, true);
+        GDP_GEMM_CASE(E_BIAS | E_GATE | E_RES, true, true);
       }
     }
     switch (epi) {                              // bf16 features too

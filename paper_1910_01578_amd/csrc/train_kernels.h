@@ -13,7 +13,7 @@
 namespace gdp {
 namespace tr {
 
-enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SIGMOID = 2 };
+enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SIGMOID = 2, ACT_GATE = 3 };   // ACT_GATE: ReLU that keeps NaN
 
 // C(m, n) = epi(sum_k A(m, k) B(k, n)) with A(m, k) = a[m sam + k sak] and
 // B(k, n) = b[k sbk + n sbn]; epi adds a bias over n (fp32 or bf16), applies

@@ -32,7 +32,8 @@ GDP_NOALLOC_SCRATCH_BYTES = 4 << 20
 KERNEL_KINDS = ["graph_prep", "nbr_sample", "gemm_pool_sigmoid", "gather_max", "gemm_update_relu",
                 "meanpool", "film", "pre_layer", "seg_attention", "post_attn",
                 "head_lse", "gumbel_sample", "logp_reduce", "mlp_placer", "ppo_grad", "head_backward", "advantages",
-                "evaluate", "train_forward", "backward", "adam", "log_prob", "gemm_update_pool"]
+                "evaluate", "train_forward", "backward", "adam", "log_prob", "gemm_update_pool", "layer_norm",
+                "layer_norm_backward", "fc", "fc_backward", "rel_attention", "rel_attention_backward"]
 K_COUNT = len(KERNEL_KINDS)
 
 
@@ -90,6 +91,19 @@ class GdpAdamTensor(ctypes.Structure):
                 ("n", c_int64)]
 
 
+class GdpFcLayer(ctypes.Structure):
+    _fields_ = [("rows", c_int64), ("in_dim", c_int32), ("out_dim", c_int32), ("dtype", c_int32), ("act", c_int32)] + \
+               [(n, c_int64) for n in ("ld_x", "ld_y", "ld_res", "ld_act", "ld_dy", "ld_dx", "ld_dx_add")]
+
+
+class GdpRelAttn(ctypes.Structure):
+    _fields_ = [("n_graphs", c_int32), ("key_start_h", POINTER(c_int32)), ("len_h", POINTER(c_int32)),
+                ("n_query_h", POINTER(c_int32)), ("n_heads", c_int32), ("n_kv_heads", c_int32),
+                ("head_dim", c_int32), ("seg_len", c_int32), ("mem_len", c_int32), ("causal", c_int32),
+                ("n_bounds", c_int32), ("bounds_h", POINTER(c_int32)), ("dtype", c_int32), ("scale", c_float)] + \
+               [(n, c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_o", "ld_do", "ld_dq", "ld_dk", "ld_dv")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_1910_01578_amd.build_lib` "
@@ -143,6 +157,18 @@ def _load():
         "gdp_debug_uniforms": (c_int32, [c_uint64, c_int32, c_int32, c_int32, c_void_p, c_void_p]),
         "gdp_debug_neighbors": (c_int32, [POINTER(GdpGraph), POINTER(GdpGnn), c_void_p, c_void_p, c_int64,
                                           c_void_p, c_size_t, c_void_p]),
+        "gdp_layer_norm": (c_int32, [c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                     c_void_p, c_float, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+        "gdp_layer_norm_workspace_bytes": (c_size_t, [c_int64, c_int32]),
+        "gdp_layer_norm_backward": (c_int32, [c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_float,
+                                              c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                              c_void_p, c_void_p, c_size_t, c_void_p]),
+        "gdp_fc": (c_int32, [POINTER(GdpFcLayer)] + [c_void_p] * 7),
+        "gdp_fc_workspace_bytes": (c_size_t, [POINTER(GdpFcLayer)]),
+        "gdp_fc_backward": (c_int32, [POINTER(GdpFcLayer)] + [c_void_p] * 9 + [c_size_t, c_void_p]),
+        "gdp_rel_attention_workspace_bytes": (c_size_t, [POINTER(GdpRelAttn), c_int32]),
+        "gdp_rel_attention": (c_int32, [POINTER(GdpRelAttn)] + [c_void_p] * 8 + [c_size_t, c_void_p]),
+        "gdp_rel_attention_backward": (c_int32, [POINTER(GdpRelAttn)] + [c_void_p] * 13 + [c_size_t, c_void_p]),
         "gdp_set_place_streams": (c_int32, [c_int32]),
         "gdp_timer_begin": (c_int32, [c_uint32]),
         "gdp_timer_end": (c_int32, [POINTER(c_double), POINTER(c_int64)]),
@@ -530,6 +556,313 @@ class RewardBaseline:
                                  self.reward_sum.data_ptr(), self.trial_count.data_ptr(), reward.data_ptr(),
                                  adv.data_ptr(), _stream_handle(stream)))
         return reward, adv
+
+
+# ----------------------------------------------------------------------------
+# Layer operators: the parts of a placement layer as calls of their own, forward
+# and backward.  Tensors are float32 or bfloat16 matrices on one GPU whose last
+# dimension is contiguous (any row stride); they run on that GPU's current
+# stream, or on `stream`, where outputs and workspaces are allocated too.
+# ----------------------------------------------------------------------------
+
+_ACTS = {"none": 0, "relu": 1}
+
+
+def _bad(msg: str):
+    raise GdpError(GDP_E_INVALID_ARG, msg)
+
+
+class _On:
+    """The tensor's GPU as the current device and, if given, a stream as its current one."""
+
+    def __init__(self, t, stream):
+        cuda = _torch().cuda
+        self.dev = None if t.device.index == cuda.current_device() else cuda.device(t.device)
+        self.st = None if stream is None else cuda.stream(stream)
+
+    def __enter__(self):
+        if self.dev is not None:
+            self.dev.__enter__()
+        if self.st is not None:
+            self.st.__enter__()
+        return int(_torch().cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *e):
+        if self.st is not None:
+            self.st.__exit__(*e)
+        if self.dev is not None:
+            self.dev.__exit__(*e)
+
+
+def _dtype_of(name, t) -> int:
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
+        return GDP_BF16
+    if t.dtype is torch.float32:
+        return GDP_F32
+    _bad(f"{name} is {t.dtype}, not float32 or bfloat16")
+
+
+def _need(name, t, like, shape, dtype=None):
+    """t has this shape, like's device, like's dtype (or the given one) and a contiguous last dimension."""
+    if t.device != like.device or t.device.type != "cuda":
+        _bad(f"{name} is on {t.device}, not on {like.device}" if t.device != like.device else f"{name} is not on a GPU")
+    if t.dtype is not (dtype or like.dtype):
+        _bad(f"{name} is {t.dtype}, not {dtype or like.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        _bad(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        _bad(f"{name}'s last dimension is not contiguous")
+    if len(shape) == 2 and 0 <= t.stride(0) < shape[1] and shape[0] > 1:
+        _bad(f"{name}'s rows overlap")
+
+
+def _ld(t) -> int:
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _dense(name, t):
+    if not t.is_contiguous():
+        _bad(f"{name} is not contiguous")
+
+
+def layer_norm(x, gamma, beta, residual=None, eps: float = 1e-5, keep_sum: bool = False, stream=None):
+    """LayerNorm of x (+ residual), [rows, width]; with keep_sum (y, sum), the sum being layer_norm_backward's h."""
+    torch = _torch()
+    dt = _dtype_of("x", x)
+    if x.dim() != 2:
+        _bad("x is not a matrix")
+    rows, width = x.shape
+    _need("x", x, x, (rows, width))
+    _need("gamma", gamma, x, (width,))
+    _need("beta", beta, x, (width,))
+    if residual is not None:
+        _need("residual", residual, x, (rows, width))
+    with _On(x, stream) as st:
+        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+        s = torch.empty_like(y) if keep_sum else None
+        check(lib.gdp_layer_norm(rows, width, dt, x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(),
+                                 0 if residual is None else _ld(residual), gamma.data_ptr(), beta.data_ptr(), float(eps),
+                                 y.data_ptr(), width, None if s is None else s.data_ptr(), width, st))
+    return (y, s) if keep_sum else y
+
+
+def layer_norm_backward(h, gamma, dy, dsum=None, eps: float = 1e-5, stream=None):
+    """The gradients of layer_norm at h (x, or the sum it kept): (dh, dgamma, dbeta), the last two fp32.  dsum: the
+    gradient that reaches h past the LayerNorm, added to dh (the gradient of x and of residual)."""
+    torch = _torch()
+    dt = _dtype_of("h", h)
+    if h.dim() != 2:
+        _bad("h is not a matrix")
+    rows, width = h.shape
+    _need("h", h, h, (rows, width))
+    _need("gamma", gamma, h, (width,))
+    _need("dy", dy, h, (rows, width))
+    if dsum is not None:
+        _need("dsum", dsum, h, (rows, width))
+    with _On(h, stream) as st:
+        dh = torch.empty((rows, width), dtype=h.dtype, device=h.device)
+        dg, db = (torch.empty(width, dtype=torch.float32, device=h.device) for _ in range(2))
+        need = lib.gdp_layer_norm_workspace_bytes(rows, width)
+        if need == 0:
+            _bad(last_error())
+        ws = torch.empty(need, dtype=torch.uint8, device=h.device)
+        check(lib.gdp_layer_norm_backward(rows, width, dt, h.data_ptr(), _ld(h), gamma.data_ptr(), float(eps),
+                                          dy.data_ptr(), _ld(dy), None if dsum is None else dsum.data_ptr(),
+                                          0 if dsum is None else _ld(dsum), dh.data_ptr(), width, dg.data_ptr(),
+                                          db.data_ptr(), ws.data_ptr(), need, st))
+    return dh, dg, db
+
+
+def fc(x, w, b=None, act: str = "none", residual=None, keep_act: bool = False, stream=None):
+    """act(x w^T + b) + residual for x [rows, K], w [N, K], act "none" or "relu"; with keep_act (y, a), a the
+    activation's output before the residual, for fc_backward (without residual that is y)."""
+    torch = _torch()
+    dt = _dtype_of("x", x)
+    if act not in _ACTS:
+        _bad(f"act {act!r} is not one of {sorted(_ACTS)}")
+    if x.dim() != 2 or w.dim() != 2:
+        _bad("x and w are not both matrices")
+    rows, k = x.shape
+    n = w.shape[0]
+    _need("x", x, x, (rows, k))
+    _need("w", w, x, (n, k))
+    _dense("w", w)
+    if b is not None:
+        _need("b", b, x, (n,))
+    if residual is not None:
+        _need("residual", residual, x, (rows, n))
+    with _On(x, stream) as st:
+        y = torch.empty((rows, n), dtype=x.dtype, device=x.device)
+        a = torch.empty_like(y) if keep_act else None
+        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), n, 0 if residual is None else _ld(residual), n, 0, 0)
+        check(lib.gdp_fc(ctypes.byref(f), x.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
+                         None if residual is None else residual.data_ptr(), y.data_ptr(),
+                         None if a is None else a.data_ptr(), st))
+    return (y, a) if keep_act else y
+
+
+def fc_backward(dy, x, w, act: str = "none", act_out=None, dx_add=None, need_dx: bool = True, stream=None):
+    """The gradients of fc: (dx or None, dw, db), the last two fp32; act_out: the activation's output (with "relu");
+    dx_add: what reaches x on another path, added to dx.  The residual's gradient is dy itself."""
+    torch = _torch()
+    dt = _dtype_of("x", x)
+    if act not in _ACTS:
+        _bad(f"act {act!r} is not one of {sorted(_ACTS)}")
+    if x.dim() != 2 or w.dim() != 2:
+        _bad("x and w are not both matrices")
+    rows, k = x.shape
+    n = w.shape[0]
+    _need("x", x, x, (rows, k))
+    _need("dy", dy, x, (rows, n))
+    _need("w", w, x, (n, k))
+    _dense("w", w)
+    if act == "relu":
+        if act_out is None:
+            _bad("act_out is needed with relu")
+        _need("act_out", act_out, x, (rows, n))
+    if dx_add is not None:
+        _need("dx_add", dx_add, x, (rows, k))
+    with _On(x, stream) as st:
+        dx = torch.empty((rows, k), dtype=x.dtype, device=x.device) if need_dx else None
+        dw = torch.empty((n, k), dtype=torch.float32, device=x.device)
+        db = torch.empty(n, dtype=torch.float32, device=x.device)
+        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), 0, 0, _ld(act_out) if act == "relu" else 0, _ld(dy), k,
+                       0 if dx_add is None else _ld(dx_add))
+        need = lib.gdp_fc_workspace_bytes(ctypes.byref(f))
+        if need == 0:
+            _bad(last_error())
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        check(lib.gdp_fc_backward(ctypes.byref(f), dy.data_ptr(), x.data_ptr(), w.data_ptr(),
+                                  act_out.data_ptr() if act == "relu" else None,
+                                  None if dx_add is None else dx_add.data_ptr(), None if dx is None else dx.data_ptr(),
+                                  dw.data_ptr(), db.data_ptr(), ws.data_ptr(), need, st))
+    return dx, dw, db
+
+
+def rel_bounds(n_buckets: int, reach: int):
+    """Bucket bounds for n_buckets buckets of a distance: one bucket a distance up to half of them, the rest
+    spread evenly over the logarithm up to `reach`, from where on the last bucket holds everything."""
+    n = int(n_buckets) - 1
+    if n < 0:
+        _bad(f"n_buckets = {n_buckets} < 1")
+    near = min(n, max(1, int(n_buckets) // 2))
+    out = list(range(1, near + 1))
+    for i in range(n - near):
+        out.append(max(out[-1] + 1, int(round(near * (reach / near) ** ((i + 1) / (n - near))))))
+    return out
+
+
+class RelAttention:
+    """Segment attention with a learned relative position bias by buckets (gdp_rel_attention) over a batch of
+    graphs.  Graph g has lengths[g] positions, whose keys and values are rows from starts[g] on (default: one graph
+    after another); queries: how many of each graph's last positions are queries (default: all; 1 for one op
+    appended to a graph whose keys and values are kept).  bounds: ascending distances at which a bucket begins.
+    The plan holds host data only: calls may run at once, on any stream or GPU."""
+
+    def __init__(self, lengths, heads: int, d_head: int, bounds, kv_heads: Optional[int] = None,
+                 seg_len: Optional[int] = None, mem_len: int = 0, causal: bool = False, queries=None, starts=None,
+                 scale: Optional[float] = None):
+        i32 = lambda a: np.array(list(a), np.int32)
+        self.lengths = i32(lengths)
+        self.starts = i32(np.cumsum(self.lengths) - self.lengths) if starts is None else i32(starts)
+        self.queries = None if queries is None else i32(queries)
+        self.bounds = i32(bounds)
+        G = self.lengths.size
+        if self.starts.size != G or (self.queries is not None and self.queries.size != G):
+            _bad("lengths, starts and queries differ in length")
+        self.heads, self.d_head = int(heads), int(d_head)
+        self.kv_heads = self.heads if kv_heads is None else int(kv_heads)
+        self.n_queries = int((self.lengths if self.queries is None else self.queries).sum())
+        self.n_buckets = (self.bounds.size + 1) * (1 if causal else 2)
+        # rows that k and v need; whether the graphs' rows cover all of them
+        self.n_rows = int((self.starts + self.lengths)[self.lengths > 0].max(initial=0))
+        self.n_keys = int(self.lengths.sum())
+        seg = max(1, int(self.lengths.max(initial=1))) if seg_len is None else int(seg_len)
+        ptr = lambda a: None if a is None else a.ctypes.data_as(POINTER(c_int32))
+        self._c = GdpRelAttn(G, ptr(self.starts), ptr(self.lengths), ptr(self.queries), self.heads, self.kv_heads,
+                             self.d_head, seg, int(mem_len), 1 if causal else 0, self.bounds.size, ptr(self.bounds),
+                             GDP_F32, self.d_head ** -0.5 if scale is None else float(scale))
+        wq, wk = self.heads * self.d_head, self.kv_heads * self.d_head
+        self._widths = (wq, wk)
+        for n, w in (("ld_q", wq), ("ld_k", wk), ("ld_v", wk), ("ld_o", wq), ("ld_do", wq), ("ld_dq", wq),
+                     ("ld_dk", wk), ("ld_dv", wk)):
+            setattr(self._c, n, w)
+        self._ws = [lib.gdp_rel_attention_workspace_bytes(ctypes.byref(self._c), 0)]
+        if self._ws[0] == 0:
+            raise GdpError(GDP_E_INVALID_ARG, last_error())
+
+    def _call(self, q, k, v, table, key_mask):
+        """The arrays checked; a descriptor of this call's own."""
+        wq, wk = self._widths
+        dt = _dtype_of("q", q)
+        if k.dim() != 2 or k.shape[0] < self.n_rows:
+            _bad(f"k has shape {tuple(k.shape)}, not at least {self.n_rows} rows of {wk}")
+        _need("q", q, q, (self.n_queries, wq))
+        _need("k", k, q, (k.shape[0], wk))
+        _need("v", v, q, (k.shape[0], wk))
+        _need("table", table, q, (self.heads, self.n_buckets))
+        _dense("table", table)
+        if key_mask is not None:
+            _need("key_mask", key_mask, q, (k.shape[0],), _torch().uint8)
+        c = GdpRelAttn.from_buffer_copy(self._c)
+        c.dtype, c.ld_q, c.ld_k, c.ld_v = dt, _ld(q), _ld(k), _ld(v)
+        return c
+
+    def _workspace(self, c, backward):
+        # sizes differ with the type in the backward alone
+        need = lib.gdp_rel_attention_workspace_bytes(ctypes.byref(c), 1) if backward else self._ws[0]
+        if need == 0:
+            raise GdpError(GDP_E_INVALID_ARG, last_error())
+        return need
+
+    def forward(self, q, k, v, table, key_mask=None, stream=None):
+        """q [queries, heads * d_head]; k, v [rows, kv_heads * d_head]; table [heads, buckets]; key_mask [rows]
+        uint8.  Returns (o like q, lse [queries, heads] fp32 in base 2, for backward)."""
+        torch = _torch()
+        c = self._call(q, k, v, table, key_mask)
+        with _On(q, stream) as st:
+            o = torch.empty((self.n_queries, self._widths[0]), dtype=q.dtype, device=q.device)
+            lse = torch.empty((self.n_queries, self.heads), dtype=torch.float32, device=q.device)
+            need = self._workspace(c, False)
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            check(lib.gdp_rel_attention(ctypes.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                                        None if key_mask is None else key_mask.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                        ws.data_ptr(), need, st))
+        return o, lse
+
+    def backward(self, dout, q, k, v, table, o, lse, key_mask=None, out=None, stream=None):
+        """(dq, dk, dv, dtable) for dL/do, from the forward's inputs and results; dtable is fp32, rows of k and v
+        that belong to no graph get zeros.  out: the arrays for dq, dk and dv (e.g. columns of one matrix), whose
+        rows of no graph are left as they are."""
+        torch = _torch()
+        c = self._call(q, k, v, table, key_mask)
+        wq, wk = self._widths
+        _need("dout", dout, q, (self.n_queries, wq))
+        _need("o", o, q, (self.n_queries, wq))
+        _need("lse", lse, q, (self.n_queries, self.heads), torch.float32)
+        _dense("lse", lse)
+        if out is not None:
+            for n, t, shape in zip(("dq", "dk", "dv"), out, (q.shape, k.shape, k.shape)):
+                _need(n, t, q, shape)
+        c.ld_do, c.ld_o = _ld(dout), _ld(o)
+        with _On(q, stream) as st:
+            if out is None:
+                make = torch.empty if self.n_keys == k.shape[0] else torch.zeros
+                dq = torch.empty((self.n_queries, wq), dtype=q.dtype, device=q.device)
+                dk, dv = (make((k.shape[0], wk), dtype=q.dtype, device=q.device) for _ in range(2))
+            else:
+                dq, dk, dv = out
+                c.ld_dq, c.ld_dk, c.ld_dv = _ld(dq), _ld(dk), _ld(dv)
+            dtable = torch.empty((self.heads, self.n_buckets), dtype=torch.float32, device=q.device)
+            need = self._workspace(c, True)
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            check(lib.gdp_rel_attention_backward(ctypes.byref(c), dout.data_ptr(), q.data_ptr(), k.data_ptr(),
+                                                 v.data_ptr(), table.data_ptr(),
+                                                 None if key_mask is None else key_mask.data_ptr(), o.data_ptr(),
+                                                 lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                                 dtable.data_ptr(), ws.data_ptr(), need, st))
+        return dq, dk, dv, dtable
 
 
 def debug_uniforms(seed: int, n: int, k: int, d: int, device="cuda", stream=None):

@@ -1,0 +1,548 @@
+"""The layer operators (layer_norm, fc, RelAttention and the layer made of them) against their definitions in
+float64, at sizes and masks where they can go wrong; bounds in operator_refs.py."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from tests import operator_refs as R
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F64 = torch.float32, torch.bfloat16, torch.float64
+TYPES = [BF16, F32]
+
+
+def _gdp():
+    from paper_1910_01578_amd import gdp
+    return gdp
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _normal(g, *shape, dtype=F32, scale=1.0, shift=0.0):
+    return (torch.randn(*shape, generator=g) * scale + shift).to(dtype)
+
+
+def _rows(t, pad):
+    """t on the GPU as columns of a wider matrix (row stride width + pad)."""
+    wide = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device="cuda")
+    wide[:, :t.shape[1]] = t.cuda()
+    return wide[:, :t.shape[1]]
+
+
+def _say(*a):
+    print(*a, flush=True)
+
+
+# ---- LayerNorm ---------------------------------------------------------------
+
+NORMS = [(0, 64), (1, 1), (3, 7), (257, 8), (65, 64), (33, 65), (129, 256), (70, 257), (40, 513), (37, 1001), (9, 1024),
+         (19, 2047), (11, 4096), (5, 4099), (3, 8192)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width", NORMS)
+def test_norm(rows, width, dtype):
+    gdp = _gdp()
+    _say("norm", rows, width, dtype)
+    g = _gen(rows * 10007 + width)
+    x, res = _normal(g, rows, width, dtype=dtype, shift=0.5), _normal(g, rows, width, dtype=dtype)
+    gamma, beta = _normal(g, width, dtype=dtype, shift=1.0, scale=0.2), _normal(g, width, dtype=dtype, scale=0.2)
+    dy = _normal(g, rows, width, dtype=dtype)
+    for residual, pad in ((None, 0), (res, 3)):
+        X, RES = _rows(x, pad), None if residual is None else _rows(residual, 2 * pad)
+        (y, by), (h, bh) = R.norm(x, gamma, beta, residual, 1e-5, dtype)
+        got, s = gdp.layer_norm(X, gamma.cuda(), beta.cuda(), residual=RES, keep_sum=True)
+        R.within(got, y, by, "y")
+        R.within(s, h, bh, "sum")
+        assert torch.equal(gdp.layer_norm(X, gamma.cuda(), beta.cuda(), residual=RES), got)
+        hd = s.cpu()
+        want = R.norm_backward(hd, gamma, dy, residual, 1e-5, dtype)
+        dh, dg, db = gdp.layer_norm_backward(s, gamma.cuda(), _rows(dy, pad), dsum=RES)
+        assert dg.dtype == db.dtype == F32
+        for name, a, (v, b) in zip(("dh", "dgamma", "dbeta"), (dh, dg, db), want):
+            R.within(a, v, b, name)
+
+
+def test_norm_many_rows_and_non_finite_ones():
+    """More rows than work-groups; a row with NaN or infinity spoils its own results only."""
+    gdp = _gdp()
+    g = _gen(1)
+    x, gamma, beta = _normal(g, 20011, 72, dtype=BF16), _normal(g, 72, dtype=BF16, shift=1.0), _normal(g, 72, dtype=BF16)
+    x[5, 3], x[77, 0], x[20010, 71] = math.nan, math.inf, -math.inf
+    y = gdp.layer_norm(x.cuda(), gamma.cuda(), beta.cuda()).cpu()
+    bad = torch.zeros(20011, dtype=torch.bool)
+    bad[[5, 77, 20010]] = True
+    assert torch.isnan(y[bad]).all()
+    (ref, bound), _ = R.norm(x[~bad], gamma, beta, None, 1e-5, BF16)
+    R.within(y[~bad], ref, bound, "y")
+    dy = _normal(g, 20011, 72, dtype=BF16)
+    x[bad] = 1.0
+    (_, _), (dg, bg), (db, bb) = R.norm_backward(x, gamma, dy, None, 1e-5, BF16)
+    _, got_g, got_b = gdp.layer_norm_backward(x.cuda(), gamma.cuda(), dy.cuda())
+    R.within(got_g, dg, bg, "dgamma")
+    R.within(got_b, db, bb, "dbeta")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_norm_in_place(dtype):
+    """y over residual, the sum over x; dh over dy."""
+    gdp = _gdp()
+    lib, p = gdp.lib, lambda t: t.data_ptr()
+    g = _gen(2)
+    dt = gdp.GDP_BF16 if dtype == BF16 else gdp.GDP_F32
+    for width in (100, 3000):
+        x, res, gamma, beta = (_normal(g, *s, dtype=dtype).cuda() for s in ((50, width), (50, width), (width,), (width,)))
+        y, s = gdp.layer_norm(x, gamma, beta, residual=res, keep_sum=True)
+        x2, r2 = x.clone(), res.clone()
+        st = torch.cuda.current_stream().cuda_stream
+        gdp.check(lib.gdp_layer_norm(50, width, dt, p(x2), width, p(r2), width, p(gamma), p(beta), 1e-5, p(r2), width, p(x2),
+                                     width, st))
+        assert torch.equal(r2, y) and torch.equal(x2, s)
+        dh, dg, db = gdp.layer_norm_backward(s, gamma, x, dsum=res)
+        d2, g2, b2 = x.clone(), torch.empty_like(dg), torch.empty_like(db)
+        n = lib.gdp_layer_norm_workspace_bytes(50, width)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        gdp.check(lib.gdp_layer_norm_backward(50, width, dt, p(s), width, p(gamma), 1e-5, p(d2), width, p(res), width, p(d2),
+                                              width, p(g2), p(b2), p(ws), n, st))
+        assert torch.equal(d2, dh) and torch.equal(g2, dg) and torch.equal(b2, db)
+
+
+# ---- FC --------------------------------------------------------------------------
+
+FCS = [(0, 16, 16), (1, 1, 1), (1, 256, 1024), (5, 31, 7), (16, 100, 17), (17, 64, 130), (33, 520, 40), (64, 33, 128),
+       (65, 1, 3), (65, 64, 64), (129, 7, 129), (130, 256, 128), (200, 72, 264), (300, 131, 517), (1000, 520, 1), (257, 1024, 4)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,n", FCS)
+def test_fc(rows, k, n, dtype):
+    gdp = _gdp()
+    _say("fc", rows, k, n, dtype)
+    g = _gen(rows * 101 + k * 7 + n)
+    x, w, b = _normal(g, rows, k, dtype=dtype), _normal(g, n, k, dtype=dtype, scale=k ** -0.5), _normal(g, n, dtype=dtype)
+    res, dy, add = _normal(g, rows, n, dtype=dtype), _normal(g, rows, n, dtype=dtype), _normal(g, rows, k, dtype=dtype)
+    W, B = w.cuda(), b.cuda()
+    for act, bias, residual, pad in (("none", None, None, 0), ("relu", b, None, 0), ("none", b, res, 8), ("relu", None, res, 5),
+                                     ("relu", b, res, 1)):
+        X, RES = _rows(x, pad), None if residual is None else _rows(residual, pad)
+        (y, by), (a, ba) = R.fc(x, w, bias, act, residual, dtype)
+        bd = None if bias is None else B
+        got, kept = gdp.fc(X, W, bd, act=act, residual=RES, keep_act=True)
+        R.within(got, y, by, f"y {act} {pad}")
+        R.within(kept, a, ba, f"a {act} {pad}")
+        alone = gdp.fc(X, W, bd, act=act, residual=RES)
+        R.within(alone, y, by, f"y alone {act} {pad}")
+        want = R.fc_backward(dy, x, w, act, kept.cpu(), add if pad else None, dtype)
+        dx, dw, db = gdp.fc_backward(_rows(dy, pad), X, W, act=act, act_out=kept if act == "relu" else None,
+                                     dx_add=_rows(add, pad) if pad else None)
+        for name, t, (v, bound) in zip(("dx", "dw", "db"), (dx, dw, db), want):
+            R.within(t, v, bound, f"{name} {act} {pad}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_fc_long_sum_over_rows(dtype):
+    """dw and db over many rows: pieces of rows joined, no row lost or taken twice."""
+    gdp = _gdp()
+    g = _gen(5)
+    for rows, k, n in ((30011, 40, 24), (9000, 264, 136)):
+        x, dy, w = _normal(g, rows, k, dtype=dtype), _normal(g, rows, n, dtype=dtype), _normal(g, n, k, dtype=dtype)
+        (dx, bx), (dw, bw), (db, bb) = R.fc_backward(dy, x, w, "none", None, None, dtype)
+        got = gdp.fc_backward(dy.cuda(), x.cuda(), w.cuda())
+        # pieces of at most 2,048 rows in fp32, those in double: their terms bound the error, not all rows
+        for name, t, v, b in zip(("dx", "dw", "db"), got, (dx, dw, db), (bx, bw * 2100 / rows, bb * 2100 / rows)):
+            R.within(t, v, b, f"{name} {rows}")
+        assert gdp.fc_backward(dy.cuda(), x.cuda(), w.cuda(), need_dx=False)[0] is None
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [7, 200])
+def test_fc_non_finite(rows, dtype):
+    """NaN passes the activation; an infinity reaches its own row only."""
+    gdp = _gdp()
+    g = _gen(6)
+    x, w = _normal(g, rows, 96, dtype=dtype), _normal(g, 64, 96, dtype=dtype)
+    x[3, 5], x[5, 95] = math.nan, math.inf
+    y = gdp.fc(x.cuda(), w.cuda(), None, act="relu").cpu()
+    assert torch.isnan(y[3]).all()
+    assert torch.equal(y[5] == math.inf, w[:, 95].float() > 0) and (y[5][w[:, 95].float() < 0] == 0).all()
+    ok = torch.ones(rows, dtype=torch.bool)
+    ok[[3, 5]] = False
+    (ref, bound), _ = R.fc(x[ok], w, None, "relu", None, dtype)
+    R.within(y[ok], ref, bound, "y")
+
+
+# ---- attention ---------------------------------------------------------------------
+
+def _attn(**kw):
+    base = dict(lengths=[100], heads=4, d_head=32, bounds=[1, 2, 4, 8, 16, 40])
+    base.update(kw)
+    return base
+
+
+ATTNS = {
+    "one key": _attn(lengths=[1]),
+    "empty and one": _attn(lengths=[0, 1, 0, 66, 2, 0], heads=2, causal=True),
+    "whole": _attn(lengths=[200]),
+    "segments": _attn(lengths=[300, 77], seg_len=64, mem_len=64),
+    "odd segments": _attn(lengths=[201, 5, 130], seg_len=33, mem_len=50, d_head=16),
+    "short segments": _attn(lengths=[150], seg_len=5, mem_len=3, d_head=16, heads=2),
+    "segments of one": _attn(lengths=[90], seg_len=1, mem_len=0, heads=1, causal=True),
+    "causal": _attn(lengths=[257], causal=True, d_head=64),
+    "causal segments": _attn(lengths=[190, 64], seg_len=40, mem_len=1000, causal=True),
+    "shared heads": _attn(lengths=[130, 70], heads=6, kv_heads=2, d_head=16, seg_len=48, mem_len=16),
+    "one shared head": _attn(lengths=[140], heads=5, kv_heads=1, d_head=64, causal=True),
+    "no bounds": _attn(lengths=[130], bounds=[]),
+    "far bounds": _attn(lengths=[300], bounds=[70, 100, 230, 500], heads=2),
+    "every distance": _attn(lengths=[129], bounds=list(range(1, 64)), heads=2, seg_len=70, mem_len=30),
+    "one query": _attn(lengths=[700, 3, 64], queries=[1, 1, 1], causal=True, kv_heads=2, d_head=64),
+    "one query of one key": _attn(lengths=[1, 1], queries=[1, 1]),
+    "few queries": _attn(lengths=[500, 40, 1200], queries=[5, 0, 17], heads=4, kv_heads=2, seg_len=600, mem_len=300),
+    "few queries over segments": _attn(lengths=[210, 99], queries=[64, 30], seg_len=20, mem_len=13, causal=True, d_head=16),
+    "65 queries": _attn(lengths=[210, 99], queries=[65, 30], seg_len=50, mem_len=13, heads=2),
+    "many parts": _attn(lengths=[9000], queries=[3], heads=2, bounds=[1, 2, 3, 50, 400, 4000], causal=True),
+    "two columns": _attn(lengths=[1000, 150], heads=64, d_head=16, seg_len=64, mem_len=32, bounds=[1, 3, 9, 30]),
+    "two columns, shared": _attn(lengths=[1030], heads=128, kv_heads=64, seg_len=100, mem_len=20, causal=True),
+    "two columns, wide": _attn(lengths=[1030], heads=64, d_head=64, seg_len=500, mem_len=100),
+}
+
+
+def _attn_inputs(case, dtype, seed, rows=None, table_scale=0.7):
+    g = _gen(seed)
+    ref = R.Attention(**case)
+    nq = sum(ref.queries)
+    rows = rows or max([s + n for s, n in zip(ref.starts, ref.lengths)] + [1])
+    q = _normal(g, nq, ref.heads * ref.d, dtype=dtype, scale=1.5)
+    k, v = (_normal(g, rows, ref.kv * ref.d, dtype=dtype) for _ in range(2))
+    table = _normal(g, ref.heads, ref.buckets, dtype=dtype, scale=table_scale)
+    do = _normal(g, nq, ref.heads * ref.d, dtype=dtype)
+    return ref, q, k, v, table, do
+
+
+def _check_attn(case, dtype, q, k, v, table, do, mask=None, pad=0, ref=None):
+    gdp = _gdp()
+    ref = ref or R.Attention(**case)
+    want = ref.run(q, k, v, table, mask, do, dtype)
+    plan = gdp.RelAttention(**case)
+    Q, K, V, DO = (_rows(t, pad) for t in (q, k, v, do))
+    T, M = table.cuda(), None if mask is None else mask.cuda()
+    o, lse = plan.forward(Q, K, V, T, key_mask=M)
+    R.within(o, *want["o"], "o")
+    R.within(lse, *want["lse"], "lse")
+    got = plan.backward(DO, Q, K, V, T, o, lse, key_mask=M)
+    assert got[3].dtype == F32
+    for name, t in zip(("dq", "dk", "dv", "dtable"), got):
+        R.within(t, *want[name], name)
+    return o, lse, got
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", list(ATTNS))
+def test_attention(name, dtype):
+    _say("attention", name, dtype)
+    ref, q, k, v, table, do = _attn_inputs(ATTNS[name], dtype, 11)
+    _check_attn(ATTNS[name], dtype, q, k, v, table, do, pad=3, ref=ref)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ["whole", "segments", "odd segments", "causal", "shared heads", "few queries", "one query",
+                                  "65 queries", "two columns"])
+def test_attention_masked(name, dtype):
+    """A key mask that leaves rows empty, with NaN and infinities in the rows that it hides."""
+    _say("masked", name, dtype)
+    ref, q, k, v, table, do = _attn_inputs(ATTNS[name], dtype, 12)
+    g = _gen(13)
+    mask = (torch.rand(k.shape[0], generator=g) < 0.6).to(torch.uint8)
+    start, n = ref.starts[0], ref.lengths[0]
+    mask[start:start + min(n, 70)] = 0                     # the first segments see nothing (causal: the first ops)
+    if len(ref.lengths) > 1:
+        mask[ref.starts[-1]:ref.starts[-1] + ref.lengths[-1]] = 0   # a graph of padding
+    hidden = mask == 0
+    k[hidden], v[hidden] = math.nan, math.inf
+    v[hidden][::2] = math.nan
+    o, lse, (dq, dk, dv, _) = _check_attn(ATTNS[name], dtype, q, k, v, table, do, mask=mask, ref=ref)
+    none = torch.isinf(lse).cpu()
+    heads = o.view(o.shape[0], ref.heads, -1).cpu()
+    assert (heads[none] == 0).all() and (dq.view_as(o).cpu().view_as(heads)[none] == 0).all()
+    assert (dk.cpu()[hidden] == 0).all() and (dv.cpu()[hidden] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ["causal", "segments", "few queries over segments"])
+def test_attention_unseen_rows(name, dtype):
+    """NaN in a key, value or query that others' rows do not see: a later op (causal), another segment."""
+    ref, q, k, v, table, do = _attn_inputs(ATTNS[name], dtype, 14)
+    gdp = _gdp()
+    _say("unseen", name, dtype)
+    n, nq = ref.lengths[0], ref.queries[0]
+    at = n - 2                                             # of the last segment; seen by the last positions only
+    clean = ref.run(q, k, v, table, None, do, dtype)
+    k[at], v[at] = math.nan, math.inf
+    T = table.cuda()
+    plan = gdp.RelAttention(**ATTNS[name])
+    o, lse = plan.forward(q.cuda(), k.cuda(), v.cuda(), T)
+    p = torch.arange(n - nq, n)
+    s0 = p // ref.seg * ref.seg
+    sees = (at >= s0 - ref.mem) & (at < s0 + ref.seg) & ((at <= p) if ref.causal else torch.ones_like(p, dtype=torch.bool))
+    assert torch.isnan(o[:nq][sees.cuda()]).all()
+    other = torch.cat([~sees, torch.ones(q.shape[0] - nq, dtype=torch.bool)])
+    for got, (ref_v, ref_b), what in ((o, clean["o"], "o"), (lse, clean["lse"], "lse")):
+        R.within(got[other.cuda()], ref_v[other], ref_b[other], what)
+    dq = plan.backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), T, o, lse)[0]
+    R.within(dq[other.cuda()], clean["dq"][0][other], clean["dq"][1][other], "dq")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ["whole", "few queries", "causal segments"])
+def test_attention_excluded_buckets_and_large_scores(name, dtype):
+    """Table entries of -inf and of the type's lowest value exclude their buckets; scores of hundreds."""
+    ref, q, k, v, table, do = _attn_inputs(ATTNS[name], dtype, 15, table_scale=40.0)
+    table[0, 1] = -math.inf
+    table[1, 2] = torch.finfo(dtype).min
+    table[2, :] = -math.inf                                # a head that sees nothing
+    o, _, (dq, _, _, dtab) = _check_attn(ATTNS[name], dtype, q * 4, k, v, table, do, ref=ref)
+    c = slice(2 * ref.d, 3 * ref.d)
+    assert (o[:, c] == 0).all() and (dq[:, c] == 0).all() and (dtab[2] == 0).all() and dtab[0, 1] == 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_rows_behind_and_order(dtype):
+    """Caches longer than their graphs and not in order: rows of no graph are neither read nor written."""
+    gdp = _gdp()
+    case = _attn(lengths=[130, 1, 70], starts=[200, 340, 10], seg_len=50, mem_len=50)
+    ref, q, k, v, table, do = _attn_inputs(case, dtype, 16, rows=400)
+    free = torch.ones(400, dtype=torch.bool)
+    for s, n in zip(ref.starts, ref.lengths):
+        free[s:s + n] = False
+    k[free], v[free] = math.nan, math.nan
+    o, lse, (_, dk, dv, _) = _check_attn(case, dtype, q, k, v, table, do, ref=ref)
+    assert (dk.cpu()[free] == 0).all() and (dv.cpu()[free] == 0).all()
+    out = (torch.empty_like(q).cuda(), torch.full((400, 128), 7.0, dtype=dtype, device="cuda"),
+           torch.full((400, 128), 7.0, dtype=dtype, device="cuda"))
+    gdp.RelAttention(**case).backward(do.cuda(), q.cuda(), k.cuda(), v.cuda(), table.cuda(), o, lse, out=out)
+    assert (out[1].cpu()[free] == 7).all() and (out[2].cpu()[free] == 7).all()
+    assert torch.equal(out[1].cpu()[~free], dk.cpu()[~free])
+
+
+@pytest.mark.parametrize("queries", [1, 100])
+def test_attention_far_rows(queries):
+    """Cache rows whose element offsets pass 2^31 and 2^32."""
+    rows, width = (1 << 26) + 600, 4 * 16
+    case = _attn(lengths=[300, 300], starts=[(1 << 25) + 3, (1 << 26) + 250], queries=[queries] * 2, d_head=16, seg_len=64,
+                 mem_len=64)
+    gdp = _gdp()
+    g = _gen(17)
+    ref = R.Attention(**case)
+    k, v = (torch.empty(rows, width, dtype=BF16, device="cuda") for _ in range(2))
+    small = [torch.empty(600, width, dtype=BF16) for _ in range(2)]
+    for t, s in zip((k, v), small):
+        for i, start in enumerate(ref.starts):
+            part = _normal(g, 300, width, dtype=BF16)
+            t[start:start + 300] = part.cuda()
+            s[300 * i:300 * i + 300] = part
+    q, do, table = _normal(g, 2 * queries, width, dtype=BF16), _normal(g, 2 * queries, width, dtype=BF16), _normal(g, 4, 14, dtype=BF16)
+    near = R.Attention(**{**case, "starts": [0, 300]})
+    want = near.run(q, small[0], small[1], table, None, do, BF16)
+    plan = gdp.RelAttention(**case)
+    o, lse = plan.forward(q.cuda(), k, v, table.cuda())
+    R.within(o, *want["o"], "o")
+    dk, dv = torch.empty_like(k), torch.empty_like(v)
+    plan.backward(do.cuda(), q.cuda(), k, v, table.cuda(), o, lse, out=(torch.empty_like(o), dk, dv))
+    for name, t in (("dk", dk), ("dv", dv)):
+        got = torch.cat([t[s:s + 300] for s in ref.starts])
+        R.within(got, *want[name], name)
+
+
+@pytest.mark.parametrize("name", ["segments", "shared heads", "causal"])
+def test_attention_gradients_against_differences(name):
+    """Each gradient along a random direction against central differences of the definition in float64."""
+    gdp = _gdp()
+    ref, q, k, v, table, do = _attn_inputs(ATTNS[name], F32, 18)
+    plan = gdp.RelAttention(**ATTNS[name])
+    args = [t.cuda() for t in (q, k, v, table)]
+    o, lse = plan.forward(*args)
+    grads = plan.backward(do.cuda(), *args, o, lse)
+    bounds = ref.run(q, k, v, table, None, do, F32)
+    g = _gen(19)
+    step = 1e-5
+    for i, (name_, x) in enumerate(zip(("dq", "dk", "dv", "dtable"), (q, k, v, table))):
+        d = torch.randn(x.shape, generator=g, dtype=F64)
+
+        def loss(sign):
+            a = [t.to(F64) for t in (q, k, v, table)]
+            a[i] = a[i] + sign * step * d
+            return float((ref.run(*a)["o"][0] * do.to(F64)).sum())
+        diff = (loss(1) - loss(-1)) / (2 * step)
+        mine = float((grads[i].cpu().to(F64) * d).sum())
+        # the gradient's own bound, and the differences': step^2 / 6 times a third derivative, taken as 100 times the size
+        tol = float((bounds[name_][1] * d.abs()).sum()) + 100 * step ** 2 * float((bounds[name_][0].abs() * d.abs()).sum()) + 1e-7
+        assert abs(diff - mine) <= tol, (name_, diff, mine, tol)
+
+
+# ---- a layer of them, streams, graphs ----------------------------------------------
+
+def _layer(dtype, seed=21, d=96, ff=200, heads=6, kv=2):
+    from paper_1910_01578_amd import rel_layer
+    gdp = _gdp()
+    g = _gen(seed)
+    case = dict(lengths=[150, 61], heads=heads, d_head=16, kv_heads=kv, bounds=gdp.rel_bounds(8, 50), seg_len=64, mem_len=32)
+    qkv = (heads + 2 * kv) * 16
+    shapes = {"w_qkv": (qkv, d), "b_qkv": (qkv,), "w_o": (d, heads * 16), "b_o": (d,), "ln1_g": (d,), "ln1_b": (d,),
+              "w_1": (ff, d), "b_1": (ff,), "w_2": (d, ff), "b_2": (d,), "ln2_g": (d,), "ln2_b": (d,), "rel_table": (heads, 16)}
+    w = {n: _normal(g, *s, dtype=dtype, scale=s[1] ** -0.5 if n.startswith("w_") else 0.3, shift=1.0 if n.endswith("_g") else 0.0)
+         for n, s in shapes.items()}
+    x, dout = _normal(g, 211, d, dtype=dtype), _normal(g, 211, d, dtype=dtype)
+    layer = rel_layer.RelPlacerLayer(gdp.RelAttention(**case), {n: t.cuda() for n, t in w.items()})
+    return layer, case, w, x, dout
+
+
+def _layer_ref(case, w, x, dout, live):
+    """The layer in float64 with autograd, its ReLU passing what `live` says: out, dx, gradients."""
+    ref = R.Attention(**case)
+    w = {n: t.to(F64).requires_grad_() for n, t in w.items()}
+    x = x.to(F64).requires_grad_()
+    ln = lambda t, a, b: (t - t.mean(1, keepdim=True)) / (t.var(1, keepdim=True, correction=0) + 1e-5).sqrt() * w[a] + w[b]
+    qkv = x @ w["w_qkv"].t() + w["b_qkv"]
+    a, b = ref.heads * ref.d, (ref.heads + ref.kv) * ref.d
+    outs, start = [], 0
+    for n in ref.lengths:
+        p, j = torch.arange(n)[:, None], torch.arange(n)[None]
+        s0 = p // ref.seg * ref.seg
+        seen = (j >= s0 - ref.mem) & (j < s0 + ref.seg)
+        rows, heads = slice(start, start + n), []
+        for h in range(ref.heads):
+            kh = h // (ref.heads // ref.kv) * ref.d
+            q, k, v = qkv[rows, h * ref.d:(h + 1) * ref.d], qkv[rows, a + kh:a + kh + ref.d], qkv[rows, b + kh:b + kh + ref.d]
+            z = q @ k.t() * ref.scale + w["rel_table"][h][ref.bucket(j - p)]
+            heads.append(torch.softmax(z.masked_fill(~seen, -math.inf), 1) @ v)
+        outs.append(torch.cat(heads, 1))
+        start += n
+    z = ln(x + torch.cat(outs) @ w["w_o"].t() + w["b_o"], "ln1_g", "ln1_b")
+    out = ln(z + ((z @ w["w_1"].t() + w["b_1"]) * live) @ w["w_2"].t() + w["b_2"], "ln2_g", "ln2_b")
+    out.backward(dout.to(F64))
+    return out.detach(), x.grad, {n: t.grad for n, t in w.items()}
+
+
+def _rel(got, ref):
+    got = got.detach().cpu().to(F64)
+    return float((got - ref).norm() / ref.norm())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer(dtype):
+    """A whole layer forward and backward.  Its activations pass 7 roundings forward and 7 backward (bf16: of rms at
+    most 2^-8, in fp32 sums of a few hundred terms, each off by less than 64 u of the result), a LayerNorm's or
+    softmax's gradient magnifies relative errors by less than 4.  The definition takes ReLU's decisions from the
+    layer's own forward: one taken the other way near zero is no rounding of a gradient."""
+    layer, case, w, x, dout = _layer(dtype)
+    out, kept = layer.forward(x.cuda())
+    dx, grads = layer.backward(dout.cuda(), kept)
+    ref_out, ref_dx, ref_g = _layer_ref(case, w, x, dout, (kept["a"] > 0).cpu())
+    step = 2.0 ** -8 if dtype == BF16 else 64 * R.U
+    tol = 4 * math.sqrt(14) * step
+    assert _rel(out, ref_out) <= tol
+    assert _rel(dx, ref_dx) <= tol
+    assert set(grads) == set(ref_g)
+    for n, t in grads.items():
+        assert t.dtype == F32
+        if n == "b_qkv":                                   # the keys' bias has no gradient: sums that cancel
+            q, kv = 6 * 16, 2 * 16
+            t, r = torch.cat([t[:q], t[q + kv:]]), torch.cat([ref_g[n][:q], ref_g[n][q + kv:]])
+            assert _rel(t, r) <= tol, n
+        else:
+            assert _rel(t, ref_g[n]) <= tol, n
+
+
+def _bits(ts):
+    return [t.detach().contiguous().view(torch.uint8).cpu().numpy().tobytes() for t in ts]
+
+
+def _all_calls(dtype):
+    """Every operator in each direction on fixed inputs; returns a function that runs them, and what it may change."""
+    gdp = _gdp()
+    layer, _, _, x, dout = _layer(dtype)
+    X, DO = x.cuda(), dout.cuda()
+    few = gdp.RelAttention([3000, 500], 6, 16, [1, 2, 5, 30, 700], kv_heads=2, causal=True, queries=[1, 3])
+    g = _gen(31)
+    q, k, v, t = (_normal(g, *s, dtype=dtype).cuda() for s in ((4, 96), (3500, 32), (3500, 32), (6, 6)))
+    res = _normal(g, 211, 200, dtype=dtype).cuda()
+
+    def run():
+        out, kept = layer.forward(X)
+        dx, grads = layer.backward(DO, kept)
+        y, a = gdp.fc(X, layer.w["w_1"], layer.w["b_1"], act="relu", residual=res, keep_act=True)
+        one = gdp.fc(X[:1], layer.w["w_1"], layer.w["b_1"], act="relu")
+        return [out, dx, *grads.values(), *few.forward(q, k, v, t), y, a, one]
+    return run, X
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_same_bits_again_and_on_other_streams(dtype):
+    run, _ = _all_calls(dtype)
+    ref = _bits(run())
+    assert _bits(run()) == ref
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for s in streams:                                      # both in flight at once
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs.append(run())
+    torch.cuda.synchronize()
+    assert all(_bits(o) == ref for o in outs)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_graph_replays(dtype):
+    """Two captured graphs replayed with eager work and new inputs between the replays."""
+    run, X = _all_calls(dtype)
+    x0 = X.clone()
+    first = _bits(run())
+    X.mul_(0.5)
+    second = _bits(run())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = run()
+        graphs.append((g, out))
+    for rep in range(3):
+        X.copy_(x0 if rep % 2 == 0 else x0 * 0.5)
+        run()
+        torch.cuda.synchronize()
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert _bits(out) == (first if rep % 2 == 0 else second), rep
+
+
+def test_stream_argument():
+    gdp = _gdp()
+    s = torch.cuda.Stream()
+    x = torch.randn(300, 64, device="cuda")
+    g, b = torch.ones(64, device="cuda"), torch.zeros(64, device="cuda")
+    want = gdp.layer_norm(x, g, b)
+    s.wait_stream(torch.cuda.current_stream())
+    got = gdp.layer_norm(x, g, b, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
+
+
+def test_event_timer_names_the_operators():
+    gdp = _gdp()
+    run, _ = _all_calls(BF16)
+    kinds = ["layer_norm", "layer_norm_backward", "fc", "fc_backward", "rel_attention", "rel_attention_backward"]
+    gdp.timer_begin(kinds)
+    run()
+    got = gdp.timer_end()
+    assert set(got) == set(kinds) and all(v["ms"] > 0 for v in got.values())
+    assert ctypes.sizeof(gdp.GdpRelAttn) > 0
