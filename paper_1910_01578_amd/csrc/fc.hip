@@ -5,10 +5,10 @@
 //
 // fp32 goes through the update step's products (train_gemm.hip: three bf16 planes an
 // operand).  bf16 has two kernels here:
-//   k_fc_tile  128 x 128 tiles, 4 waves of 64 x 64, k in steps of 64 through two LDS
-//              buffers filled by direct loads one step ahead.  The operands stay in
-//              their memory order; one whose contraction dimension is not the fast one
-//              (W in dx, both in dW) is read by transposing LDS reads.
+//   k_fc_tile  128 x 128 or 256 x 256 tiles, k in stages of 32 filled by direct loads.
+//              The operands stay in their memory order; one whose contraction dimension
+//              is not the fast one (W in dx, both in dW) is read by transposing LDS reads.
+//              (k_fc_any: the same through registers, for operands of odd alignment.)
 //   k_fc_few   up to 64 rows: 16 outputs a work-group, k dealt to its 8 waves, no LDS
 //              but for the waves' sums.  What bounds it: reading W.
 // Both add in fp32 and round once.  dP has no rounding of its own (a selection), so dW
@@ -26,72 +26,13 @@ namespace op {
 
 namespace {
 
-constexpr int kBM = 128, kBK = 64;
-constexpr int kTileBytes = kBM * kBK * 2;
-
-// One operand's tile: 128 rows (of C's rows or columns) x 64 k.  TR false: k is the fast
-// dimension, an LDS row is 64 k of one row; true: an LDS row is 128 rows of one k.
-// 16-byte granules of an LDS row are permuted so that fragment reads (plain: 16 rows x 4
-// granules; transposing: rows {8 g + 0..3} x 2 granules) fall in distinct banks.
-template <bool TR>
-struct OpTile {
-  static constexpr int GPR = TR ? kBM / 8 : kBK / 8, PER = 4;
-  static __device__ __forceinline__ int key(int r) { return TR ? ((r & 3) | ((r >> 1) & 4)) << 1 : r & 7; }
-  const bf16* base;                    // the tile's first element at k = 0
-  int64_t ld;
-  int rows, K;                         // rows left from the tile's first; contraction length
-  uint32_t off[PER];                   // of this lane's granules in one full step, bytes
-  static __device__ __forceinline__ int pos(int i) { return ((int)(threadIdx.x >> 6) * PER + i) * 64 + (int)(threadIdx.x & 63); }
-  static __device__ __forceinline__ int row(int i) { return pos(i) / GPR; }
-  static __device__ __forceinline__ int gran(int i) { return (pos(i) % GPR) ^ key(row(i)); }
-  __device__ __forceinline__ OpTile(const bf16* p, int64_t ld_, int rows_, int K_) : base(p), ld(ld_), rows(rows_), K(K_) {
-    // past the edge: the last row (granule) again, its results are not stored
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      off[i] = TR ? (uint32_t)(((int64_t)row(i) * ld + min(gran(i) * 8, (rows - 1) & ~7)) * 2)
-                  : (uint32_t)(((int64_t)min(row(i), rows - 1) * ld + gran(i) * 8) * 2);
-  }
-  __device__ __forceinline__ void dma(char* lds, int step) const {
-    const dma::gptr_t b = dma::uniform_base(base + (int64_t)step * kBK * (TR ? ld : 1));
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) dma::dma16(b, off[i], lds + (wave * PER + i) * 1024);
-  }
-  // any alignment, zeros past the contraction's end
-  Vec16<bf16> v[PER];
-  __device__ __forceinline__ void load(int step) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int k = step * kBK + (TR ? row(i) : gran(i) * 8), r = TR ? gran(i) * 8 : min(row(i), rows - 1);
-      const int left = TR ? (k < K ? rows - r : 0) : K - k;
-      const bf16* p = base + (TR ? (int64_t)k * ld + r : (int64_t)r * ld + k);
-      if (left > 0) v[i] = load16_part(p, left);
-      else *reinterpret_cast<uint4*>(&v[i]) = make_uint4(0, 0, 0, 0);
-    }
-  }
-  __device__ __forceinline__ void store(char* lds) const {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) *reinterpret_cast<uint4*>(lds + pos(i) * 16) = *reinterpret_cast<const uint4*>(&v[i]);
-  }
-  // rows r0 + (lane & 15), k = 32 ks + 8 (lane / 16) + [0, 8)
-  static __device__ __forceinline__ bf16x8 frag(const char* lds, int r0, int ks, int col, int g4) {
-    if constexpr (!TR) {
-      const int r = r0 + col;
-      return *reinterpret_cast<const bf16x8*>(lds + r * 128 + (((ks * 4 + g4) ^ key(r)) << 4));
-    } else {
-      const int k = 32 * ks + 8 * g4 + (col >> 2), c = r0 + 4 * (col & 3);
-      const char* p = lds + (c % 8) * 2;
-      return join8(read_tr16(p + k * 256 + (((c / 8) ^ key(k)) << 4)), read_tr16(p + (k + 4) * 256 + (((c / 8) ^ key(k + 4)) << 4)));
-    }
-  }
-};
-
 // C(m, n) = sum_k A(m, k) B(n, k).
 struct FcProduct {
-  const bf16 *a, *b;
-  int64_t lda, ldb;
+  const bf16 *a, *b, *gate;            // gate (or NULL): A's elements count where it is above 0
+  int64_t lda, ldb, ldgate;
   int M, N, K;
-  int mt, nt, k_per_split;             // tiles; contraction length of one split (a multiple of 64)
+  int mt, nt;                          // tiles
+  int splits, k_per_split;             // pieces of the contraction
   // epilogue of bf16 results
   const bf16 *bias, *res;
   int64_t ldr;
@@ -102,164 +43,328 @@ struct FcProduct {
   float *f, *rowsum;
 };
 
-template <bool ATR, bool BTR, bool DMA>
-__global__ __launch_bounds__(256, 2) void k_fc_tile(FcProduct g) {
+constexpr int kStep = 32;              // k of one LDS stage
+__device__ const uint4 kZeros = {0, 0, 0, 0};
+
+// One operand's stage in LDS: R rows x 32 k.  TR false: k is the fast dimension, an LDS
+// row is 32 k of one row; true: an LDS row is R rows of one k.  16-byte granules of an LDS
+// row are permuted so that fragment reads (plain: 16 rows x 4 granules; transposing: rows
+// {8 g + 0..3} x 2 granules) fall in distinct banks.
+template <bool TR, int R, int NT>
+struct OpTile {
+  static constexpr int GPR = TR ? R / 8 : kStep / 8, PER = R * kStep / 8 / NT, kBytes = R * kStep * 2;
+  static __device__ __forceinline__ int key(int r) { return TR ? ((r & 3) | ((r >> 1) & 4)) << 1 : ((r >> 2) ^ (r >> 1)) & 3; }
+  static __device__ __forceinline__ int pos(int i) { return ((int)(threadIdx.x >> 6) * PER + i) * 64 + (int)(threadIdx.x & 63); }
+  static __device__ __forceinline__ int row(int i) { return pos(i) / GPR; }
+  static __device__ __forceinline__ int gran(int i) { return (pos(i) % GPR) ^ key(row(i)); }
+  // rows r0 + (lane & 15), k = 8 (lane / 16) + [0, 8)
+  static __device__ __forceinline__ bf16x8 frag(const char* lds, int r0, int col, int g4) {
+    if constexpr (!TR) {
+      const int r = r0 + col;
+      return *reinterpret_cast<const bf16x8*>(lds + r * (kStep * 2) + ((g4 ^ key(r)) << 4));
+    } else {
+      const int k = 8 * g4 + (col >> 2), c = r0 + 4 * (col & 3);
+      const char* p = lds + (c % 8) * 2;
+      return join8(read_tr16(p + k * (R * 2) + (((c / 8) ^ key(k)) << 4)), read_tr16(p + (k + 4) * (R * 2) + (((c / 8) ^ key(k + 4)) << 4)));
+    }
+  }
+};
+
+// bf16 values of x where g is above 0 (NaN is not), else 0: packed 16-bit integer
+// operations on the bits, as the values above 0 are 0x0001 .. 0x7f80.
+__device__ __forceinline__ bf16x8 gated(const bf16x8& x, const bf16x8& g) {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+  union V {
+    bf16x8 q;
+    u16x2 h[4];
+    uint32_t u[4];
+  } v, m;
+  v.q = x;
+  m.q = g;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const u16x2 t = __builtin_elementwise_min((u16x2)(m.h[i] - (uint16_t)1), (u16x2)(uint16_t)0x7f80) - (uint16_t)0x7f80;
+    const i16x2 keep = __builtin_bit_cast(i16x2, t) >> (int16_t)15;
+    v.u[i] &= __builtin_bit_cast(uint32_t, keep);
+  }
+  return v.q;
+}
+
+// A WM x WN block of C in a wave's registers: 16 x 16 blocks formed transposed, so that a
+// lane holds 4 consecutive columns of one row.
+template <int WM, int WN, bool F32>
+struct Block {
+  static constexpr int NI = WM / 16, NJ = WN / 16;
+  f32x4 acc[NI][NJ], ones[F32 ? NI : 1];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = zero4();
+#pragma unroll
+    for (int i = 0; i < (F32 ? NI : 1); ++i) ones[i] = zero4();
+  }
+  // one stage; sums: rowsum too
+  template <typename TA, typename TB>
+  __device__ __forceinline__ void step(const char* sa, const char* sb, const char* sg, int mw, int nw, int col, int g4, bool sums) {
+    bf16x8 fa[NI], fb[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[j] = TB::frag(sb, nw + 16 * j, col, g4);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      fa[i] = TA::frag(sa, mw + 16 * i, col, g4);
+      if (sg) fa[i] = gated(fa[i], TA::frag(sg, mw + 16 * i, col, g4));
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = mma16(fb[j], fa[i], acc[i][j]);
+    if constexpr (F32) {
+      if (sums) {
+        bf16x8 one;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) one[e] = (bf16)1.0f;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) ones[i] = mma16(one, fa[i], ones[i]);
+      }
+    }
+  }
+  // Bias, activation, residual and stores.  Two neighbouring 16 x 16 blocks exchange lane
+  // rows so that a lane holds 8 consecutive columns: 16-byte accesses, 64 bytes a row.
+  __device__ __forceinline__ void store(const FcProduct& g, int m0, int n0, int z, int col, int g4, bool sums) const {
+    float bias[NJ][4];
+    if constexpr (!F32) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int n = n0 + 16 * j + 4 * g4 + r;
+          bias[j][r] = g.bias && n < g.N ? to_f32(g.bias[n]) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int m = m0 + 16 * i + col;
+#pragma unroll
+      for (int jp = 0; jp < NJ / 2; ++jp) {
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = acc[i][2 * jp][r] + (F32 ? 0.f : bias[2 * jp][r]), y = acc[i][2 * jp + 1][r] + (F32 ? 0.f : bias[2 * jp + 1][r]);
+          const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
+          const uint32_t own = t[0], other = t[1];         // (a bit cast of the element itself takes element 0)
+          v[r] = __builtin_bit_cast(float, own);
+          v[4 + r] = __builtin_bit_cast(float, other);
+        }
+        const int n = n0 + 32 * jp + 16 * (g4 & 1) + 8 * (g4 >> 1), left = g.N - n;
+        if (m >= g.M || left <= 0) continue;
+        if constexpr (F32) {
+          float* p = g.f + ((int64_t)z * g.M + m) * g.N + n;
+          Vec16<float> lo, hi;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            lo.v[e] = v[e];
+            hi.v[e] = v[4 + e];
+          }
+          store16_part(p, lo, left);
+          if (left > 4) store16_part(p + 4, hi, left - 4);
+        } else {
+          Vec16<bf16> o;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            if (g.relu) v[e] = v[e] < 0.f ? 0.f : v[e];    // NaN stays
+            o.v[e] = (bf16)v[e];
+          }
+          if (g.act_out) store16_part(g.act_out + (int64_t)m * g.ldact + n, o, left);
+          if (g.res) {
+            const Vec16<bf16> r = load16_part(g.res + (int64_t)m * g.ldr + n, left);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o.v[e] = (bf16)(v[e] + to_f32(r.v[e]));
+          }
+          store16_part(g.c + (int64_t)m * g.ldc + n, o, left);
+        }
+      }
+      if constexpr (F32) {
+        if (sums && g4 == 0 && m < g.M) g.rowsum[(int64_t)z * g.M + m] = ones[i][0];
+      }
+    }
+  }
+};
+
+// Tile t of the product, columns first, then rows, then pieces: neighbours share A's rows
+// (dW: the rows of both).
+template <int BM, int BN>
+struct TileAt {
+  int m0, n0, z, kb, K;
+  __device__ __forceinline__ TileAt(const FcProduct& g, int t) {
+    n0 = t % g.nt * BN;
+    m0 = t / g.nt % g.mt * BM;
+    z = t / (g.nt * g.mt);
+    kb = z * g.k_per_split;
+    K = min(g.K - kb, g.k_per_split);
+  }
+};
+
+// Aligned operands.  A work-group walks its tiles in one stream of 32-k stages: direct
+// loads run NS - 1 stages ahead of the matrix instructions, across the ends of tiles, so
+// that a short contraction does not wait for its first loads and its epilogue overlaps the
+// next tile's.  A stage past the contraction's end reads zeros.
+template <bool ATR, bool BTR, bool GATE, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProduct g, int tiles) {
+  constexpr int NT = BM / WM * (BN / WN) * 64;
   constexpr bool F32 = ATR;            // dW
-  __shared__ __attribute__((aligned(1024))) char lds[4 * kTileBytes];
+  using TA = OpTile<ATR, BM, NT>;
+  using TB = OpTile<BTR, BN, NT>;
+  constexpr int kStage = TA::kBytes * (GATE ? 2 : 1) + TB::kBytes, kLoads = TA::PER * (GATE ? 2 : 1) + TB::PER;
+  __shared__ __attribute__((aligned(1024))) char lds[NS * kStage];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g4 = lane >> 4;
+  const int mw = wave / (BN / WN) * WM, nw = wave % (BN / WN) * WN;
+  // each XCD takes a run of tiles, its work-groups take them in turn
+  const int groups = (int)gridDim.x / kNumXcd, xcd = blockIdx.x % kNumXcd;
+  const int per = tiles / kNumXcd, rem = tiles % kNumXcd;
+  const int t_end = (xcd + 1) * per + min(xcd + 1, rem);
+  const int t_first = xcd * per + min(xcd, rem) + (int)blockIdx.x / kNumXcd;
+  if (t_first >= t_end) return;
+
+  // where the loads are: tile lt, stage ls of it
+  int lt = t_first, ls = 0, lsteps = 0, lk = 0;
+  const bf16 *pa = nullptr, *pb = nullptr, *pg = nullptr;
+  uint32_t oa[TA::PER], ob[TB::PER], og[TA::PER];
+  auto aim = [&]() {
+    const TileAt<BM, BN> t(g, lt);
+    lsteps = (t.K + kStep - 1) / kStep;
+    lk = t.K;
+    ls = 0;
+    auto offsets = [&](auto tile, int64_t ld, int rows, auto& off) {
+      using O = decltype(tile);
+      // past the edge: the last row (granule) again, its results are not stored
+#pragma unroll
+      for (int i = 0; i < O::PER; ++i)
+        off[i] = O::GPR > 4 ? (uint32_t)((O::row(i) * ld + min(O::gran(i) * 8, (rows - 1) & ~7)) * 2)
+                            : (uint32_t)((min(O::row(i), rows - 1) * ld + O::gran(i) * 8) * 2);
+    };
+    pa = g.a + (ATR ? (int64_t)t.kb * g.lda + t.m0 : (int64_t)t.m0 * g.lda + t.kb);
+    pb = g.b + (BTR ? (int64_t)t.kb * g.ldb + t.n0 : (int64_t)t.n0 * g.ldb + t.kb);
+    offsets(TA(), g.lda, g.M - t.m0, oa);
+    offsets(TB(), g.ldb, g.N - t.n0, ob);
+    if constexpr (GATE) {
+      pg = g.gate + (ATR ? (int64_t)t.kb * g.ldgate + t.m0 : (int64_t)t.m0 * g.ldgate + t.kb);
+      offsets(TA(), g.ldgate, g.M - t.m0, og);
+    }
+  };
+  auto fetch = [&](int slot) {                             // the next stage; past the last one: that one again
+    char* to = lds + slot * kStage;
+    auto load = [&](auto tile, const bf16* p, int64_t ld, const auto& off, char* at) {
+      using O = decltype(tile);
+      const bf16* q = p + (int64_t)ls * kStep * (O::GPR > 4 ? ld : 1);
+      if ((ls + 1) * kStep <= lk) {
+        const dma::gptr_t base = dma::uniform_base(q);
+#pragma unroll
+        for (int i = 0; i < O::PER; ++i) dma::dma16(base, off[i], at + (wave * O::PER + i) * 1024);
+      } else {
+        const int left = lk - ls * kStep;
+#pragma unroll
+        for (int i = 0; i < O::PER; ++i) {
+          const bool in = (O::GPR > 4 ? O::row(i) : O::gran(i) * 8) < left;
+          dma::dma16_lane(in ? reinterpret_cast<const char*>(q) + off[i] : reinterpret_cast<const char*>(&kZeros), at + (wave * O::PER + i) * 1024);
+        }
+      }
+    };
+    load(TA(), pa, g.lda, oa, to);
+    load(TB(), pb, g.ldb, ob, to + TA::kBytes);
+    if constexpr (GATE) load(TA(), pg, g.ldgate, og, to + TA::kBytes + TB::kBytes);
+    if (ls + 1 < lsteps) ++ls;
+    else if (lt + groups < t_end) {
+      lt += groups;
+      aim();
+    }
+  };
+  aim();
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) fetch(s);
+  int slot = 0;
+  Block<WM, WN, F32> b;
+  for (int t = t_first; t < t_end; t += groups) {
+    const TileAt<BM, BN> at(g, t);
+    const int steps = (at.K + kStep - 1) / kStep;
+    const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
+    b.clear();
+    for (int s = 0; s < steps; ++s) {
+      // this stage's loads are in (NS - 2 stages are younger), the last stage has been read
+      dma::wait_vm_barrier<(NS - 2) * kLoads>();
+      fetch(slot == 0 ? NS - 1 : slot - 1);
+      const char* p = lds + slot * kStage;
+      b.template step<TA, TB>(p, p + TA::kBytes, GATE ? p + TA::kBytes + TB::kBytes : nullptr, mw, nw, col, g4, sums);
+      slot = slot == NS - 1 ? 0 : slot + 1;
+    }
+    b.store(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
+  }
+  dma::wait_loads_then_barrier();                          // no direct load outlives the work-group
+}
+
+// Operands of any alignment and contraction length: 128 x 128 tiles, stages through
+// registers, two LDS buffers.
+template <bool ATR, bool BTR>
+__global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
+  constexpr int BT = 128;
+  constexpr bool F32 = ATR;
+  using TA = OpTile<ATR, BT, 256>;
+  using TB = OpTile<BTR, BT, 256>;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * (TA::kBytes + TB::kBytes)];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
   const int mw = (wave >> 1) * 64, nw = (wave & 1) * 64;
-  // consecutive tiles share A's rows (dW: the rows of both): keep them on one XCD
-  const int tile = xcd_remap(blockIdx.x, gridDim.x);
-  const int n0 = tile % g.nt * kBM, m0 = tile / g.nt % g.mt * kBM, z = tile / (g.nt * g.mt);
-  const int kb = z * g.k_per_split, K = min(g.K - kb, g.k_per_split);
-  OpTile<ATR> A(g.a + (ATR ? (int64_t)kb * g.lda + m0 : (int64_t)m0 * g.lda + kb), g.lda, g.M - m0, K);
-  OpTile<BTR> B(g.b + (BTR ? (int64_t)kb * g.ldb + n0 : (int64_t)n0 * g.ldb + kb), g.ldb, g.N - n0, K);
-  f32x4 acc[4][4], ones_acc[F32 ? 4 : 1];
+  const TileAt<BT, BT> at(g, xcd_remap(blockIdx.x, gridDim.x));
+  const bf16* pa = g.a + (ATR ? (int64_t)at.kb * g.lda + at.m0 : (int64_t)at.m0 * g.lda + at.kb);
+  const bf16* pb = g.b + (BTR ? (int64_t)at.kb * g.ldb + at.n0 : (int64_t)at.n0 * g.ldb + at.kb);
+  const bf16* pg = g.gate ? g.gate + (ATR ? (int64_t)at.kb * g.ldgate + at.m0 : (int64_t)at.m0 * g.ldgate + at.kb) : nullptr;
+  Vec16<bf16> va[TA::PER], vb[TB::PER];
+  auto load = [&](auto tile, const bf16* p, int64_t ld, int rows, int s, auto& v) {
+    using O = decltype(tile);
+    constexpr bool TR = O::GPR > 4;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < O::PER; ++i) {
+      const int k = s * kStep + (TR ? O::row(i) : O::gran(i) * 8), r = TR ? O::gran(i) * 8 : min(O::row(i), rows - 1);
+      const int left = TR ? (k < at.K ? rows - r : 0) : at.K - k;
+      if (left > 0) v[i] = load16_part(p + (TR ? (int64_t)k * ld + r : (int64_t)r * ld + k), left);
+      else *reinterpret_cast<uint4*>(&v[i]) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto fetch = [&](int s) {
+    load(TA(), pa, g.lda, g.M - at.m0, s, va);
+    load(TB(), pb, g.ldb, g.N - at.n0, s, vb);
+    if (pg) {
+      Vec16<bf16> vg[TA::PER];
+      load(TA(), pg, g.ldgate, g.M - at.m0, s, vg);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = zero4();
-  const bool sums = F32 && g.rowsum && n0 == 0 && nw == 0;
-  bf16x8 one;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) one[i] = (bf16)1.0f;
-#pragma unroll
-  for (int i = 0; i < (F32 ? 4 : 1); ++i) ones_acc[i] = zero4();
-  auto buf_a = [&](int s) { return lds + (s & 1) * 2 * kTileBytes; };
-  auto compute = [&](int s) {
-    const char *sa = buf_a(s), *sb = sa + kTileBytes;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 fa[4], fb[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) fa[i] = OpTile<ATR>::frag(sa, mw + 16 * i, ks, col, g4);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) fb[j] = OpTile<BTR>::frag(sb, nw + 16 * j, ks, col, g4);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mma16(fb[j], fa[i], acc[i][j]);
-      if constexpr (F32) {
-        if (sums) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) ones_acc[i] = mma16(one, fa[i], ones_acc[i]);
-        }
+      for (int i = 0; i < TA::PER; ++i) {
+        const bf16x8 t = gated(as_bf16x8(va[i]), as_bf16x8(vg[i]));
+        va[i] = __builtin_bit_cast(Vec16<bf16>, t);
       }
     }
   };
-  if constexpr (DMA) {
-    const int full = K / kBK;
-    if (full > 0) {
-      A.dma(buf_a(0), 0);
-      B.dma(buf_a(0) + kTileBytes, 0);
-    }
-    for (int s = 0; s < full; ++s) {
-      dma::wait_loads_then_barrier();                      // step s is in; step s - 1 has been read
-      if (s + 1 < full) {
-        A.dma(buf_a(s + 1), s + 1);
-        B.dma(buf_a(s + 1) + kTileBytes, s + 1);
-      }
-      compute(s);
-    }
-    if (K % kBK) {                                         // the rest through registers, with zeros
-      A.load(full);
-      B.load(full);
-      A.store(buf_a(full));
-      B.store(buf_a(full) + kTileBytes);
-      __syncthreads();
-      compute(full);
-    }
-  } else {
-    const int steps = (K + kBK - 1) / kBK;
-    A.load(0);
-    B.load(0);
-    A.store(buf_a(0));
-    B.store(buf_a(0) + kTileBytes);
-    if (steps > 1) {
-      A.load(1);
-      B.load(1);
-    }
-    for (int s = 0; s < steps; ++s) {
-      __syncthreads();
-      if (s + 1 < steps) {
-        A.store(buf_a(s + 1));
-        B.store(buf_a(s + 1) + kTileBytes);
-      }
-      if (s + 2 < steps) {
-        A.load(s + 2);
-        B.load(s + 2);
-      }
-      compute(s);
-    }
+  auto put = [&](int s) {
+    char* p = lds + (s & 1) * (TA::kBytes + TB::kBytes);
+#pragma unroll
+    for (int i = 0; i < TA::PER; ++i) *reinterpret_cast<uint4*>(p + TA::pos(i) * 16) = *reinterpret_cast<const uint4*>(&va[i]);
+#pragma unroll
+    for (int i = 0; i < TB::PER; ++i) *reinterpret_cast<uint4*>(p + TA::kBytes + TB::pos(i) * 16) = *reinterpret_cast<const uint4*>(&vb[i]);
+  };
+  const int steps = (at.K + kStep - 1) / kStep;
+  const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
+  Block<64, 64, F32> b;
+  b.clear();
+  fetch(0);
+  put(0);
+  if (steps > 1) fetch(1);
+  for (int s = 0; s < steps; ++s) {
+    __syncthreads();
+    if (s + 1 < steps) put(s + 1);
+    if (s + 2 < steps) fetch(s + 2);
+    const char* p = lds + (s & 1) * (TA::kBytes + TB::kBytes);
+    b.template step<TA, TB>(p, p + TA::kBytes, nullptr, mw, nw, col, g4, sums);
   }
-  __syncthreads();
-  // Each wave turns its 64 x 64 block through its quarter of LDS, so that a lane holds 8
-  // consecutive columns and 8 lanes a row's 64.
-  char* mine = lds + wave * (64 * 64 * 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = 16 * i + col;
-      *reinterpret_cast<f32x4*>(mine + m * 256 + (((4 * j + g4) ^ (m & 15)) << 4)) = acc[i][j];
-    }
-  __syncthreads();
-  const int n = n0 + nw + (lane & 7) * 8, left = g.N - n;
-  float bias[8];
-  if constexpr (!F32) {
-    const Vec16<bf16> t = g.bias && left > 0 ? load16_part(g.bias + n, left) : Vec16<bf16>{};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = to_f32(t.v[e]);
-  }
-  if (left > 0) {
-#pragma unroll 2
-    for (int t = 0; t < 8; ++t) {
-      const int ml = t * 8 + (lane >> 3), m = m0 + mw + ml;
-      if (m >= g.M) break;
-      float v[8];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(mine + ml * 256 + (((2 * (lane & 7) + h) ^ (ml & 15)) << 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
-      }
-      if constexpr (F32) {
-        float* p = g.f + ((int64_t)z * g.M + m) * g.N + n;
-        Vec16<float> lo, hi;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          lo.v[e] = v[e];
-          hi.v[e] = v[4 + e];
-        }
-        store16_part(p, lo, left);
-        if (left > 4) store16_part(p + 4, hi, left - 4);
-      } else {
-        Vec16<bf16> o;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          v[e] += bias[e];
-          if (g.relu) v[e] = v[e] < 0.f ? 0.f : v[e];      // NaN stays
-          o.v[e] = (bf16)v[e];
-        }
-        if (g.act_out) store16_part(g.act_out + (int64_t)m * g.ldact + n, o, left);
-        if (g.res) {
-          const Vec16<bf16> r = load16_part(g.res + (int64_t)m * g.ldr + n, left);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o.v[e] = (bf16)(v[e] + to_f32(r.v[e]));
-        }
-        store16_part(g.c + (int64_t)m * g.ldc + n, o, left);
-      }
-    }
-  }
-  if constexpr (F32) {
-    if (sums && g4 == 0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = m0 + mw + 16 * i + col;
-        if (m < g.M) g.rowsum[(int64_t)z * g.M + m] = ones_acc[i][0];
-      }
-    }
-  }
+  b.store(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
 }
 
 // The splits' sums in order, in double.  entries of dW, then of db.
@@ -278,20 +383,17 @@ __global__ __launch_bounds__(256) void k_fc_join(const float* __restrict__ f, co
   else db[i - mn] = (float)t;
 }
 
-// dP = dy where act_out > 0 (act_out NULL: dy), rows of ldp elements with zeros behind the N-th.
-template <typename T>
-__global__ __launch_bounds__(256) void k_fc_mask(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ a, int64_t lda,
-                                                 int64_t rows, int N, T* __restrict__ dp, int64_t ldp) {
-  constexpr int V = Vec16<T>::N;
-  const int64_t per = ldp / V, total = rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / per;
-    const int n = (int)(i - r * per) * V;
-    Vec16<T> t = load16_part(dy + r * lddy + n, N - n);
+// fp32: dP = dy where act_out > 0 (act_out NULL: dy), rows of ldp elements with zeros behind the N-th.
+__global__ __launch_bounds__(256) void k_fc_mask(const float* __restrict__ dy, int64_t lddy, const float* __restrict__ a, int64_t lda,
+                                                 int rows, int N, float* __restrict__ dp, int64_t ldp) {
+  const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4;
+  if (n >= ldp) return;
+  for (int64_t r = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.y * 4) {
+    Vec16<float> t = load16_part(dy + r * lddy + n, N - n);
     if (a) {
-      const Vec16<T> x = load16_part(a + r * lda + n, N - n);
+      const Vec16<float> x = load16_part(a + r * lda + n, N - n);
 #pragma unroll
-      for (int e = 0; e < V; ++e) t.v[e] = to_f32(x.v[e]) > 0.f ? t.v[e] : (T)0.f;
+      for (int e = 0; e < 4; ++e) t.v[e] = x.v[e] > 0.f ? t.v[e] : 0.f;
     }
     store16(dp + r * ldp + n, t);
   }
@@ -387,15 +489,38 @@ bool dma_ok(const bf16* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld %
 // The same where the granules run along `cols` columns: the last one is whole.
 bool dma_ok(const bf16* p, int64_t ld, int cols) { return dma_ok(p, ld) && cols % 8 == 0; }
 
+// Large tiles (256 x 256, 8 waves, one work-group a CU) read LDS less per product, where
+// they fill the chip.
 template <bool ATR, bool BTR>
-hipError_t launch_tile(const FcProduct& g, int splits, bool dma, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)g.mt * g.nt * splits)), block(256);
-  if (dma) hipLaunchKernelGGL((k_fc_tile<ATR, BTR, true>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false>), grid, block, 0, s, g);
+hipError_t launch_product(FcProduct g, bool aligned, hipStream_t s) {
+  auto tiles = [&](int bm, int bn) {
+    g.mt = (g.M + bm - 1) / bm;
+    g.nt = (g.N + bn - 1) / bn;
+    return (int64_t)g.mt * g.nt * g.splits;
+  };
+  if (!aligned || (g.gate && !dma_ok(g.gate, g.ldgate))) {
+    const dim3 grid((unsigned)tiles(128, 128)), block(256);
+    hipLaunchKernelGGL((k_fc_any<ATR, BTR>), grid, block, 0, s, g);
+    return hipGetLastError();
+  }
+  if constexpr (!ATR) {
+    if (!g.gate && g.K >= 512 && tiles(256, 256) >= 256) {
+      const int n = (int)tiles(256, 256);
+      hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 256, 256, 128, 64, 4>), dim3(256), dim3(512), 0, s, g, n);
+      return hipGetLastError();
+    }
+  }
+  const int n = (int)tiles(128, 128);
+  const dim3 grid((unsigned)std::min(512, (n + kNumXcd - 1) / kNumXcd * kNumXcd)), block(256);
+  if constexpr (ATR || BTR) {
+    if (g.gate) {
+      hipLaunchKernelGGL((k_fc_tile<ATR, BTR, true, 128, 128, 64, 64, 3>), grid, block, 0, s, g, n);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 128, 128, 64, 64, 4>), grid, block, 0, s, g, n);
   return hipGetLastError();
 }
-
-int tiles_of(int n) { return (n + kBM - 1) / kBM; }
 
 }  // namespace
 
@@ -442,10 +567,8 @@ hipError_t launch_fc(const gdp_fc_layer& f, const T* x, const T* w, const T* b, 
     g.ldb = K;
     g.M = M;
     g.N = N;
-    g.K = K;
-    g.mt = tiles_of(M);
-    g.nt = tiles_of(N);
-    g.k_per_split = (K + kBK - 1) / kBK * kBK;
+    g.K = g.k_per_split = K;
+    g.splits = 1;
     g.bias = b;
     g.res = residual;
     g.ldr = f.ld_res;
@@ -454,7 +577,7 @@ hipError_t launch_fc(const gdp_fc_layer& f, const T* x, const T* w, const T* b, 
     g.act_out = act_out;
     g.ldact = f.ld_act;
     g.relu = relu;
-    return launch_tile<false, false>(g, 1, dma_ok(x, f.ld_x) && dma_ok(w, K), s);
+    return launch_product<false, false>(g, dma_ok(x, f.ld_x) && dma_ok(w, K), s);
   }
 }
 
@@ -463,18 +586,6 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
                               const T* act_out, const T* dx_add, T* dx, float* dw, float* db, void* ws, hipStream_t s) {
   const int M = (int)f.rows, K = f.in_dim, N = f.out_dim;
   char* base = static_cast<char*>(ws);
-  const T* dp = dy;
-  int64_t ldp = f.ld_dy;
-  if (p.ldp > 0 && M > 0) {
-    T* t = reinterpret_cast<T*>(base + p.dp);
-    const int64_t blocks = std::min<int64_t>((f.rows * (p.ldp / Vec16<T>::N) + 255) / 256, 8192);
-    hipLaunchKernelGGL((k_fc_mask<T>), dim3((unsigned)blocks), dim3(256), 0, s, dy, f.ld_dy,
-                       f.act == GDP_ACT_RELU ? act_out : (const T*)nullptr, f.ld_act, f.rows, N, t, p.ldp);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    dp = t;
-    ldp = p.ldp;
-  }
   float* part = reinterpret_cast<float*>(base + p.partial);
   const int64_t mn = (int64_t)N * K;
   if (M == 0) {                                            // no rows: gradients of zero
@@ -482,8 +593,19 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
                        (const float*)nullptr, 0, mn, N, dw, db);
     return hipGetLastError();
   }
+  const T* gate = f.act == GDP_ACT_RELU ? act_out : nullptr;
   if constexpr (sizeof(T) == 4) {
+    const T* dp = dy;
+    int64_t ldp = f.ld_dy;
     hipError_t e = hipSuccess;
+    if (p.ldp > 0) {
+      float* t = reinterpret_cast<float*>(base + p.dp);
+      const dim3 grid((unsigned)(p.ldp / 4 + 63) / 64, (unsigned)std::min((M + 3) / 4, 4096));
+      hipLaunchKernelGGL(k_fc_mask, grid, dim3(256), 0, s, dy, f.ld_dy, gate, f.ld_act, M, N, t, p.ldp);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      dp = t;
+      ldp = p.ldp;
+    }
     if (dx) {
       tr::GemmStrided<float, float> g = {dp, ldp, 1, w, K, 1, M, K, N, dx, f.ld_dx};
       g.res = dx_add;
@@ -496,40 +618,38 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
     g.rowsum = db;
     return tr::launch_gemm_strided(g, part, p.partial_floats, s);
   } else {
+    FcProduct g = {};
+    g.a = dy;
+    g.lda = f.ld_dy;
+    g.gate = gate;
+    g.ldgate = f.ld_act;
+    const bool rows_ok = dma_ok(dy, f.ld_dy);
     if (dx) {
-      FcProduct g = {};
-      g.a = dp;
-      g.lda = ldp;
-      g.b = w;
-      g.ldb = K;
-      g.M = M;
-      g.N = K;
-      g.K = N;
-      g.mt = tiles_of(M);
-      g.nt = tiles_of(K);
-      g.k_per_split = (N + kBK - 1) / kBK * kBK;
-      g.res = dx_add;
-      g.ldr = f.ld_dx_add;
-      g.c = dx;
-      g.ldc = f.ld_dx;
-      const hipError_t e = launch_tile<false, true>(g, 1, dma_ok(dp, ldp) && dma_ok(w, K, K), s);
+      FcProduct d = g;
+      d.b = w;
+      d.ldb = K;
+      d.M = M;
+      d.N = K;
+      d.K = d.k_per_split = N;
+      d.splits = 1;
+      d.res = dx_add;
+      d.ldr = f.ld_dx_add;
+      d.c = dx;
+      d.ldc = f.ld_dx;
+      const hipError_t e = launch_product<false, true>(d, rows_ok && N % 8 == 0 && dma_ok(w, K, K), s);
       if (e != hipSuccess) return e;
     }
     if (!dw && !db) return hipSuccess;
-    FcProduct g = {};
-    g.a = dp;
-    g.lda = ldp;
     g.b = x;
     g.ldb = f.ld_x;
     g.M = N;
     g.N = K;
     g.K = M;
-    g.mt = tiles_of(N);
-    g.nt = tiles_of(K);
+    g.splits = p.splits;
     g.k_per_split = p.rows_per_split;
     g.f = part;
     g.rowsum = part + p.splits * mn;
-    const hipError_t e = launch_tile<true, true>(g, p.splits, dma_ok(dp, ldp, p.ldp > 0 ? 8 : N) && dma_ok(x, f.ld_x, K), s);
+    const hipError_t e = launch_product<true, true>(g, rows_ok && N % 8 == 0 && dma_ok(x, f.ld_x, K), s);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_fc_join, dim3((unsigned)((mn + N + 255) / 256)), dim3(256), 0, s, (const float*)part,
                        (const float*)g.rowsum, p.splits, mn, N, dw, db);

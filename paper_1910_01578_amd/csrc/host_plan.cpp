@@ -418,11 +418,10 @@ void plan_fc_backward(const gdp_fc_layer* f, FcPlan* p) {
   carve_init(&p->c);
   const int64_t M = f->rows, K = f->in_dim, N = f->out_dim;
   const bool f32 = f->dtype == GDP_F32;
-  const int64_t vec = f32 ? 4 : 8;
-  // ReLU's gradient is a selection of dy; and the fp32 products tell a matrix's order by
-  // which stride is 1, so a column (row stride 1) is copied too
-  p->ldp = f->act == GDP_ACT_RELU || (f32 && f->ld_dy == 1) ? (N + vec - 1) / vec * vec : 0;
-  p->dp = carve_add(&p->c, (size_t)(p->ldp * M) * elem_size(f->dtype));
+  // fp32: ReLU's selection of dy, for both products; and they tell a matrix's order by which
+  // stride is 1, so a column (row stride 1) is copied too
+  p->ldp = f32 && (f->act == GDP_ACT_RELU || f->ld_dy == 1) ? (N + 3) / 4 * 4 : 0;
+  p->dp = carve_add(&p->c, (size_t)(p->ldp * M) * 4);
   if (f32) {
     const int64_t pieces = std::min<int64_t>(64, std::max<int64_t>(1, M / 256));
     p->partial_floats = (N * (K + 1) * pieces + 63) / 64 * 64;

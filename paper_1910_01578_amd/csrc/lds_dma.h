@@ -65,6 +65,12 @@ __device__ __forceinline__ void dma16(gptr_t base, uint32_t voff, const void* ld
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :: "v"(voff), "s"(base), "s"(__builtin_amdgcn_readfirstlane(la)) : "memory", "m0");
 }
+// The same from an address of each lane's own.
+__device__ __forceinline__ void dma16_lane(const void* p, const void* lds) {
+  const uint32_t la = (uint32_t)(uintptr_t)lds;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"((uint64_t)p), "s"(__builtin_amdgcn_readfirstlane(la)) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // ROWS x COLS block of a row-major matrix (leading dimension ld; rows beyond

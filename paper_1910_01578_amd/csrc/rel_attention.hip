@@ -22,9 +22,10 @@
 //
 // D: the dQ pass starts from D0 = dO . o with the given o, and forms D = sum P dP beside
 // its products, for the dK pass and dtable: a rounded o would be the largest error of
-// dtable (which sums differences whose leading parts cancel).  dq itself takes the rest,
-// (D0 - D) sum P k, from a third product (bf16: without it its error is 1.5 times a
-// rounding of the exact dq, with it 1.4).
+// dtable (which sums differences whose leading parts cancel).  For bf16 data dq takes what
+// D0 leaves, (D0 - D) sum P k, from a product of its own, and its dS as two planes: a row's
+// dS add up to zero, so the part that its keys have in common cancels and leaves their
+// roundings (with one plane dq's error was 1.5 roundings of the exact dq, so 1.1).
 //
 // A column whose result is not finite is formed again, key by key over what it sees: a
 // NaN or infinity in a row that it does not see meets a probability of zero in a tile
@@ -974,7 +975,14 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
           acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
           if constexpr (REST) {
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(tp[c]);
+            for (int c = 0; c < COLS; ++c) {
+#pragma unroll
+              for (int r = 0; r < 8; ++r) t[c][r] -= to_f32(w[c].p[0][r]);
+              w[c] = operand_of<1>(t[c]);
+            }
+            acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
+#pragma unroll
+            for (int c = 0; c < COLS; ++c) w[c] = operand_of<1>(tp[c]);
             acc_rows<T, DH, COLS>(pk, sK, 32 * h, w, col, g4);
           }
         }
