@@ -569,7 +569,8 @@ int gdp_fc(const gdp_fc_layer* f, const void* x, const void* w, const void* b, c
  *   dx_add    device [rows, K], or NULL: what reaches x on another path
  *   dx        device [rows, K] (output, may be NULL; may be dx_add)
  *   dw, db    device [N, K], [N] fp32 (outputs, each may be NULL)
- * Workspace: gdp_fc_workspace_bytes(f) (0 on invalid arguments).
+ * Workspace: gdp_fc_workspace_bytes(f) for these sizes and row strides (those of dy and
+ * x matter); 0 on invalid arguments.
  */
 size_t gdp_fc_workspace_bytes(const gdp_fc_layer* f);
 int gdp_fc_backward(const gdp_fc_layer* f, const void* dy, const void* x, const void* w, const void* act_out,

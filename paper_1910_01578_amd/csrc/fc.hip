@@ -28,8 +28,8 @@ namespace {
 
 // C(m, n) = sum_k A(m, k) B(n, k).
 struct FcProduct {
-  const bf16 *a, *b, *gate;            // gate (or NULL): A's elements count where it is above 0
-  int64_t lda, ldb, ldgate;
+  const bf16 *a, *b;
+  int64_t lda, ldb;
   int M, N, K;
   int mt, nt;                          // tiles
   int splits, k_per_split;             // pieces of the contraction
@@ -70,127 +70,129 @@ struct OpTile {
   }
 };
 
-// bf16 values of x where g is above 0 (NaN is not), else 0: packed 16-bit integer
-// operations on the bits, as the values above 0 are 0x0001 .. 0x7f80.
-__device__ __forceinline__ bf16x8 gated(const bf16x8& x, const bf16x8& g) {
-  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-  typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
-  union V {
-    bf16x8 q;
-    u16x2 h[4];
-    uint32_t u[4];
-  } v, m;
-  v.q = x;
-  m.q = g;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const u16x2 t = __builtin_elementwise_min((u16x2)(m.h[i] - (uint16_t)1), (u16x2)(uint16_t)0x7f80) - (uint16_t)0x7f80;
-    const i16x2 keep = __builtin_bit_cast(i16x2, t) >> (int16_t)15;
-    v.u[i] &= __builtin_bit_cast(uint32_t, keep);
-  }
-  return v.q;
-}
-
 // A WM x WN block of C in a wave's registers: 16 x 16 blocks formed transposed, so that a
 // lane holds 4 consecutive columns of one row.
 template <int WM, int WN, bool F32>
 struct Block {
   static constexpr int NI = WM / 16, NJ = WN / 16;
   f32x4 acc[NI][NJ], ones[F32 ? NI : 1];
-  __device__ __forceinline__ void clear() {
+  // bias(j, v): the lane's 4 columns of blocks j (bf16 results), else zeros
+  template <typename Bias>
+  __device__ __forceinline__ void clear(Bias bias) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int j = 0; j < NJ; ++j) {
+      f32x4 v = zero4();
+      if constexpr (!F32) bias(j, v);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = zero4();
+      for (int i = 0; i < NI; ++i) acc[i][j] = v;
+    }
 #pragma unroll
     for (int i = 0; i < (F32 ? NI : 1); ++i) ones[i] = zero4();
   }
-  // one stage; sums: rowsum too
-  template <typename TA, typename TB>
-  __device__ __forceinline__ void step(const char* sa, const char* sb, const char* sg, int mw, int nw, int col, int g4, bool sums) {
-    bf16x8 fa[NI], fb[NJ];
+  // row block i of one stage; sums: rowsum too
+  __device__ __forceinline__ void add(int i, const bf16x8& a, const bf16x8 (&b)[NJ], bool sums) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) fb[j] = TB::frag(sb, nw + 16 * j, col, g4);
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      fa[i] = TA::frag(sa, mw + 16 * i, col, g4);
-      if (sg) fa[i] = gated(fa[i], TA::frag(sg, mw + 16 * i, col, g4));
-    }
-#pragma unroll
-    for (int i = 0; i < NI; ++i)
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) acc[i][j] = mma16(fb[j], fa[i], acc[i][j]);
+    for (int j = 0; j < NJ; ++j) acc[i][j] = mma16(b[j], a, acc[i][j]);
     if constexpr (F32) {
       if (sums) {
         bf16x8 one;
 #pragma unroll
         for (int e = 0; e < 8; ++e) one[e] = (bf16)1.0f;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) ones[i] = mma16(one, fa[i], ones[i]);
+        ones[i] = mma16(one, a, ones[i]);
       }
     }
   }
-  // Bias, activation, residual and stores.  Two neighbouring 16 x 16 blocks exchange lane
-  // rows so that a lane holds 8 consecutive columns: 16-byte accesses, 64 bytes a row.
-  __device__ __forceinline__ void store(const FcProduct& g, int m0, int n0, int z, int col, int g4, bool sums) const {
-    float bias[NJ][4];
-    if constexpr (!F32) {
+  // Activation, residual and stores, rows from m0, columns from n0.  Two neighbouring 16 x 16
+  // blocks exchange lane rows so that a lane holds 8 consecutive columns: 16-byte accesses,
+  // 64 bytes a row.  PART: N may end inside a vector.  PLAIN: neither residual nor act_out.  A residual is loaded in
+  // batches before their stores: a load behind a store that may alias it waits.
+  template <bool PART, bool PLAIN>
+  __device__ __forceinline__ void store_as(const FcProduct& g, int m0, int n0, int z, int col, int g4, bool sums) const {
+    constexpr int NP = NJ / 2, NR = 8 / NP;                // 8 vectors of residual at a time
+    const int n = n0 + 16 * (g4 & 1) + 8 * (g4 >> 1);      // of pair 0; pair p: 32 p further
+    const float least = g.relu ? 0.f : -INFINITY;
+    bf16* c = F32 ? nullptr : g.c + (int64_t)(m0 + col) * g.ldc + n;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+    for (int h = 0; h < NI; h += NR) {
+      Vec16<bf16> res[PLAIN ? 1 : NR][PLAIN ? 1 : NP];
+      if constexpr (!PLAIN) {
+        if (g.res) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int n = n0 + 16 * j + 4 * g4 + r;
-          bias[j][r] = g.bias && n < g.N ? to_f32(g.bias[n]) : 0.f;
+          for (int i = 0; i < NR; ++i)
+#pragma unroll
+            for (int jp = 0; jp < NP; ++jp) {
+              const int m = m0 + 16 * (h + i) + col, left = g.N - n - 32 * jp;
+              if (m < g.M && left > 0) res[i][jp] = load16_part(g.res + (int64_t)m * g.ldr + n + 32 * jp, PART ? left : 8);
+            }
         }
-    }
+      }
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int m = m0 + 16 * i + col;
+      for (int i = 0; i < NR; ++i) {
+        const int m = m0 + 16 * (h + i) + col;
 #pragma unroll
-      for (int jp = 0; jp < NJ / 2; ++jp) {
-        float v[8];
+        for (int jp = 0; jp < NP; ++jp) {
+          float v[8];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float x = acc[i][2 * jp][r] + (F32 ? 0.f : bias[2 * jp][r]), y = acc[i][2 * jp + 1][r] + (F32 ? 0.f : bias[2 * jp + 1][r]);
-          const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y), false, false);
-          const uint32_t own = t[0], other = t[1];         // (a bit cast of the element itself takes element 0)
-          v[r] = __builtin_bit_cast(float, own);
-          v[4 + r] = __builtin_bit_cast(float, other);
+          for (int r = 0; r < 4; ++r) {
+            const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)acc[h + i][2 * jp][r]),
+                                                            __builtin_bit_cast(uint32_t, (float)acc[h + i][2 * jp + 1][r]), false, false);
+            const uint32_t own = t[0], other = t[1];       // (a bit cast of the element itself takes element 0)
+            v[r] = __builtin_bit_cast(float, own);
+            v[4 + r] = __builtin_bit_cast(float, other);
+          }
+          if (m >= g.M || n + 32 * jp >= g.N) continue;
+          const int left = PART ? g.N - n - 32 * jp : 8;
+          if constexpr (F32) {
+            float* p = g.f + ((int64_t)z * g.M + m) * g.N + n + 32 * jp;
+            Vec16<float> lo, hi;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              lo.v[e] = v[e];
+              hi.v[e] = v[4 + e];
+            }
+            store16_part(p, lo, left);
+            if (left > 4) store16_part(p + 4, hi, left - 4);
+          } else {
+            Vec16<bf16> o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              v[e] = __builtin_elementwise_maximum(v[e], least);             // NaN stays
+              o.v[e] = (bf16)v[e];
+            }
+            if constexpr (!PLAIN) {
+              if (g.act_out) store16_part(g.act_out + (int64_t)m * g.ldact + n + 32 * jp, o, left);
+              if (g.res) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o.v[e] = (bf16)(v[e] + to_f32(res[i][jp].v[e]));
+              }
+            }
+            store16_part(c + 32 * jp, o, left);
+          }
         }
-        const int n = n0 + 32 * jp + 16 * (g4 & 1) + 8 * (g4 >> 1), left = g.N - n;
-        if (m >= g.M || left <= 0) continue;
         if constexpr (F32) {
-          float* p = g.f + ((int64_t)z * g.M + m) * g.N + n;
-          Vec16<float> lo, hi;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            lo.v[e] = v[e];
-            hi.v[e] = v[4 + e];
-          }
-          store16_part(p, lo, left);
-          if (left > 4) store16_part(p + 4, hi, left - 4);
+          if (sums && g4 == 0 && m < g.M) g.rowsum[(int64_t)z * g.M + m] = ones[h + i][0];
         } else {
-          Vec16<bf16> o;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (g.relu) v[e] = v[e] < 0.f ? 0.f : v[e];    // NaN stays
-            o.v[e] = (bf16)v[e];
-          }
-          if (g.act_out) store16_part(g.act_out + (int64_t)m * g.ldact + n, o, left);
-          if (g.res) {
-            const Vec16<bf16> r = load16_part(g.res + (int64_t)m * g.ldr + n, left);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o.v[e] = (bf16)(v[e] + to_f32(r.v[e]));
-          }
-          store16_part(g.c + (int64_t)m * g.ldc + n, o, left);
+          c += 16 * g.ldc;
         }
       }
-      if constexpr (F32) {
-        if (sums && g4 == 0 && m < g.M) g.rowsum[(int64_t)z * g.M + m] = ones[i][0];
-      }
     }
+  }
+  template <bool PART>
+  __device__ __forceinline__ void store(const FcProduct& g, int m0, int n0, int z, int col, int g4, bool sums) const {
+    if (F32 || (!g.res && !g.act_out)) store_as<PART, true>(g, m0, n0, z, col, g4, sums);
+    else store_as<PART, false>(g, m0, n0, z, col, g4, sums);
   }
 };
+
+// Four columns' bias by single loads.
+__device__ __forceinline__ f32x4 bias_at_column(const FcProduct& g, int n) {
+  f32x4 v = zero4();
+  if (g.bias) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = to_f32(g.bias[min(n + r, g.N - 1)]);
+  }
+  return v;
+}
 
 // Tile t of the product, columns first, then rows, then pieces: neighbours share A's rows
 // (dW: the rows of both).
@@ -206,18 +208,60 @@ struct TileAt {
   }
 };
 
+// One operand's way from memory to a work-group's stages: the granules of this lane, each
+// load's place a constant past M0 and past the address alike.
+template <typename O>
+struct Feed {
+  static constexpr bool TR = O::GPR > 4;
+  static constexpr int kBack = 4096;                       // keeps 32-bit offsets less those constants positive
+  const char* p;                                           // the next stage, less kBack
+  int64_t step;                                            // bytes from stage to stage
+  uint32_t off[O::PER];
+  __device__ __forceinline__ void aim(const bf16* first, int64_t ld, int rows) {
+    p = reinterpret_cast<const char*>(first) - kBack;
+    step = TR ? ld * (kStep * 2) : kStep * 2;
+    // past the edge: the last row (granule) again, its results are not stored
+#pragma unroll
+    for (int i = 0; i < O::PER; ++i)
+      off[i] = (uint32_t)((TR ? O::row(i) * ld + min(O::gran(i) * 8, (rows - 1) & ~7) : min(O::row(i), rows - 1) * ld + O::gran(i) * 8) * 2) + kBack - i * 1024;
+  }
+  // the next stage to LDS address `to` (of this wave's first granule); left: k from there on
+  __device__ __forceinline__ void fetch(uint32_t to, int left) {
+    static_assert(O::PER == 2 || O::PER == 4, "loads a lane");
+    if (left >= kStep) {
+      const dma::gptr_t base = dma::uniform_base(p);
+      if constexpr (O::PER == 2) dma::dma16x2(base, off[0], off[1], to);
+      else dma::dma16x4(base, off[0], off[1], off[2], off[3], to);
+    } else {
+      const char* at[O::PER];
+#pragma unroll
+      for (int i = 0; i < O::PER; ++i)
+        at[i] = (TR ? O::row(i) : O::gran(i) * 8) < left ? p + off[i] : reinterpret_cast<const char*>(&kZeros) - i * 1024;
+      if constexpr (O::PER == 2) dma::dma16x2(at[0], at[1], to);
+      else dma::dma16x4(at[0], at[1], at[2], at[3], to);
+    }
+    p += step;
+  }
+};
+
 // Aligned operands.  A work-group walks its tiles in one stream of 32-k stages: direct
 // loads run NS - 1 stages ahead of the matrix instructions, across the ends of tiles, so
-// that a short contraction does not wait for its first loads and its epilogue overlaps the
-// next tile's.  A stage past the contraction's end reads zeros.
-template <bool ATR, bool BTR, bool GATE, int BM, int BN, int WM, int WN, int NS>
+// that a short contraction does not wait for its first loads and an epilogue overlaps the
+// next tile's.  A stage past the contraction's end reads zeros.  The bias comes with the
+// stages.  Fragments of A are read two row blocks ahead of their products.
+// A step is short (16 or 32 matrix instructions a wave): what it does beside them, scalar
+// instructions too, shows.  PART: the results' columns may end inside a vector (the bias then
+// comes by single loads).
+template <bool ATR, bool BTR, bool PART, int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProduct g, int tiles) {
   constexpr int NT = BM / WM * (BN / WN) * 64;
   constexpr bool F32 = ATR;            // dW
   using TA = OpTile<ATR, BM, NT>;
   using TB = OpTile<BTR, BN, NT>;
-  constexpr int kStage = TA::kBytes * (GATE ? 2 : 1) + TB::kBytes, kLoads = TA::PER * (GATE ? 2 : 1) + TB::PER;
+  constexpr int kStage = TA::kBytes + TB::kBytes, kLoads = TA::PER + TB::PER;
+  constexpr int NI = WM / 16, NJ = WN / 16;
   __shared__ __attribute__((aligned(1024))) char lds[NS * kStage];
+  __shared__ __attribute__((aligned(16))) char s_bias[2][F32 ? 16 : BN * 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g4 = lane >> 4;
   const int mw = wave / (BN / WN) * WM, nw = wave % (BN / WN) * WN;
   // each XCD takes a run of tiles, its work-groups take them in turn
@@ -227,78 +271,79 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProdu
   const int t_first = xcd * per + min(xcd, rem) + (int)blockIdx.x / kNumXcd;
   if (t_first >= t_end) return;
 
-  // where the loads are: tile lt, stage ls of it
-  int lt = t_first, ls = 0, lsteps = 0, lk = 0;
-  const bf16 *pa = nullptr, *pb = nullptr, *pg = nullptr;
-  uint32_t oa[TA::PER], ob[TB::PER], og[TA::PER];
-  auto aim = [&]() {
-    const TileAt<BM, BN> t(g, lt);
-    lsteps = (t.K + kStep - 1) / kStep;
-    lk = t.K;
-    ls = 0;
-    auto offsets = [&](auto tile, int64_t ld, int rows, auto& off) {
-      using O = decltype(tile);
-      // past the edge: the last row (granule) again, its results are not stored
-#pragma unroll
-      for (int i = 0; i < O::PER; ++i)
-        off[i] = O::GPR > 4 ? (uint32_t)((O::row(i) * ld + min(O::gran(i) * 8, (rows - 1) & ~7)) * 2)
-                            : (uint32_t)((min(O::row(i), rows - 1) * ld + O::gran(i) * 8) * 2);
-    };
-    pa = g.a + (ATR ? (int64_t)t.kb * g.lda + t.m0 : (int64_t)t.m0 * g.lda + t.kb);
-    pb = g.b + (BTR ? (int64_t)t.kb * g.ldb + t.n0 : (int64_t)t.n0 * g.ldb + t.kb);
-    offsets(TA(), g.lda, g.M - t.m0, oa);
-    offsets(TB(), g.ldb, g.N - t.n0, ob);
-    if constexpr (GATE) {
-      pg = g.gate + (ATR ? (int64_t)t.kb * g.ldgate + t.m0 : (int64_t)t.m0 * g.ldgate + t.kb);
-      offsets(TA(), g.ldgate, g.M - t.m0, og);
-    }
-  };
-  auto fetch = [&](int slot) {                             // the next stage; past the last one: that one again
-    char* to = lds + slot * kStage;
-    auto load = [&](auto tile, const bf16* p, int64_t ld, const auto& off, char* at) {
-      using O = decltype(tile);
-      const bf16* q = p + (int64_t)ls * kStep * (O::GPR > 4 ? ld : 1);
-      if ((ls + 1) * kStep <= lk) {
-        const dma::gptr_t base = dma::uniform_base(q);
-#pragma unroll
-        for (int i = 0; i < O::PER; ++i) dma::dma16(base, off[i], at + (wave * O::PER + i) * 1024);
-      } else {
-        const int left = lk - ls * kStep;
-#pragma unroll
-        for (int i = 0; i < O::PER; ++i) {
-          const bool in = (O::GPR > 4 ? O::row(i) : O::gran(i) * 8) < left;
-          dma::dma16_lane(in ? reinterpret_cast<const char*>(q) + off[i] : reinterpret_cast<const char*>(&kZeros), at + (wave * O::PER + i) * 1024);
-        }
+  Feed<TA> feed_a;
+  Feed<TB> feed_b;
+  int left = 0, parity = 0;                                // of the tile that is loaded
+  auto aim = [&](int tile) {
+    const TileAt<BM, BN> t(g, tile);
+    left = t.K;
+    feed_a.aim(g.a + (ATR ? (int64_t)t.kb * g.lda + t.m0 : (int64_t)t.m0 * g.lda + t.kb), g.lda, g.M - t.m0);
+    feed_b.aim(g.b + (BTR ? (int64_t)t.kb * g.ldb + t.n0 : (int64_t)t.n0 * g.ldb + t.kb), g.ldb, g.N - t.n0);
+    if constexpr (!F32 && !PART) {
+      if (wave == 0 && lane < BN / 8) {                    // this tile's bias, older than its first stage
+        const int n = t.n0 + lane * 8;
+        dma::dma16_lane(g.bias && n < g.N ? reinterpret_cast<const char*>(g.bias + n) : reinterpret_cast<const char*>(&kZeros), s_bias[parity]);
       }
-    };
-    load(TA(), pa, g.lda, oa, to);
-    load(TB(), pb, g.ldb, ob, to + TA::kBytes);
-    if constexpr (GATE) load(TA(), pg, g.ldgate, og, to + TA::kBytes + TB::kBytes);
-    if (ls + 1 < lsteps) ++ls;
-    else if (lt + groups < t_end) {
-      lt += groups;
-      aim();
+      parity ^= 1;
     }
   };
-  aim();
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s) fetch(s);
-  int slot = 0;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)lds;          // (a generic LDS address's low word is the LDS offset)
+  auto fetch = [&](int at) {                               // the next stage to byte `at` of the ring
+    feed_a.fetch(lds0 + at + wave * (TA::PER * 1024), left);
+    feed_b.fetch(lds0 + at + TA::kBytes + wave * (TB::PER * 1024), left);
+    left -= kStep;
+  };
+  int now = 0, free = (NS - 1) * kStage, bias_at = 0;      // the stage to be multiplied, the one before it
+  auto turn = [&]() {
+    free = now;
+    now = now == (NS - 1) * kStage ? 0 : now + kStage;
+  };
   Block<WM, WN, F32> b;
+  bf16x8 fa[4];
+  auto read_b = [&](const char* p, int j) { return TB::frag(p + TA::kBytes, nw + 16 * j, col, g4); };
+  auto step = [&](bool sums) {
+    dma::wait_vm_barrier<(NS - 2) * kLoads>();             // this stage is in, the last one has been read
+    fetch(free);
+    const char* p = lds + now;
+    bf16x8 fb[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[j] = read_b(p, j);
+    fa[0] = TA::frag(p, mw, col, g4);
+    fa[1] = TA::frag(p, mw + 16, col, g4);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      if (i + 2 < NI) fa[(i + 2) % 4] = TA::frag(p, mw + 16 * (i + 2), col, g4);
+      b.add(i, fa[i % 4], fb, sums);
+    }
+    turn();
+  };
+  aim(t_first);
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) fetch(s * kStage);
   for (int t = t_first; t < t_end; t += groups) {
     const TileAt<BM, BN> at(g, t);
-    const int steps = (at.K + kStep - 1) / kStep;
     const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
-    b.clear();
-    for (int s = 0; s < steps; ++s) {
-      // this stage's loads are in (NS - 2 stages are younger), the last stage has been read
-      dma::wait_vm_barrier<(NS - 2) * kLoads>();
-      fetch(slot == 0 ? NS - 1 : slot - 1);
-      const char* p = lds + slot * kStage;
-      b.template step<TA, TB>(p, p + TA::kBytes, GATE ? p + TA::kBytes + TB::kBytes : nullptr, mw, nw, col, g4, sums);
-      slot = slot == NS - 1 ? 0 : slot + 1;
-    }
-    b.store(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
+    b.clear([&](int j, f32x4& v) {
+      if constexpr (PART) {
+        v = bias_at_column(g, at.n0 + nw + 16 * j + 4 * g4);
+      } else {
+        union {
+          uint2 u;
+          bf16 h[4];
+        } x;
+        x.u = *reinterpret_cast<const uint2*>(s_bias[bias_at] + (nw + 16 * j + 4 * g4) * 2);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = to_f32(x.h[r]);
+      }
+    });
+    // the last NS - 1 steps load the next tile's first stages (behind the last tile: zeros)
+    const int steps = max(NS - 1, (at.K + kStep - 1) / kStep);
+    for (int s = 0; s < steps - (NS - 1); ++s) step(sums);
+    left = 0;
+    if (t + groups < t_end) aim(t + groups);
+    for (int s = 0; s < NS - 1; ++s) step(sums);
+    b.template store<PART>(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
+    bias_at ^= 1;
   }
   dma::wait_loads_then_barrier();                          // no direct load outlives the work-group
 }
@@ -317,7 +362,6 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
   const TileAt<BT, BT> at(g, xcd_remap(blockIdx.x, gridDim.x));
   const bf16* pa = g.a + (ATR ? (int64_t)at.kb * g.lda + at.m0 : (int64_t)at.m0 * g.lda + at.kb);
   const bf16* pb = g.b + (BTR ? (int64_t)at.kb * g.ldb + at.n0 : (int64_t)at.n0 * g.ldb + at.kb);
-  const bf16* pg = g.gate ? g.gate + (ATR ? (int64_t)at.kb * g.ldgate + at.m0 : (int64_t)at.m0 * g.ldgate + at.kb) : nullptr;
   Vec16<bf16> va[TA::PER], vb[TB::PER];
   auto load = [&](auto tile, const bf16* p, int64_t ld, int rows, int s, auto& v) {
     using O = decltype(tile);
@@ -333,15 +377,6 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
   auto fetch = [&](int s) {
     load(TA(), pa, g.lda, g.M - at.m0, s, va);
     load(TB(), pb, g.ldb, g.N - at.n0, s, vb);
-    if (pg) {
-      Vec16<bf16> vg[TA::PER];
-      load(TA(), pg, g.ldgate, g.M - at.m0, s, vg);
-#pragma unroll
-      for (int i = 0; i < TA::PER; ++i) {
-        const bf16x8 t = gated(as_bf16x8(va[i]), as_bf16x8(vg[i]));
-        va[i] = __builtin_bit_cast(Vec16<bf16>, t);
-      }
-    }
   };
   auto put = [&](int s) {
     char* p = lds + (s & 1) * (TA::kBytes + TB::kBytes);
@@ -353,7 +388,7 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
   const int steps = (at.K + kStep - 1) / kStep;
   const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
   Block<64, 64, F32> b;
-  b.clear();
+  b.clear([&](int j, f32x4& v) { v = bias_at_column(g, at.n0 + nw + 16 * j + 4 * g4); });
   fetch(0);
   put(0);
   if (steps > 1) fetch(1);
@@ -362,9 +397,13 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
     if (s + 1 < steps) put(s + 1);
     if (s + 2 < steps) fetch(s + 2);
     const char* p = lds + (s & 1) * (TA::kBytes + TB::kBytes);
-    b.template step<TA, TB>(p, p + TA::kBytes, nullptr, mw, nw, col, g4, sums);
+    bf16x8 fb[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fb[j] = TB::frag(p + TA::kBytes, nw + 16 * j, col, g4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b.add(i, TA::frag(p, mw + 16 * i, col, g4), fb, sums);
   }
-  b.store(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
+  b.template store<true>(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
 }
 
 // The splits' sums in order, in double.  entries of dW, then of db.
@@ -383,20 +422,47 @@ __global__ __launch_bounds__(256) void k_fc_join(const float* __restrict__ f, co
   else db[i - mn] = (float)t;
 }
 
-// fp32: dP = dy where act_out > 0 (act_out NULL: dy), rows of ldp elements with zeros behind the N-th.
-__global__ __launch_bounds__(256) void k_fc_mask(const float* __restrict__ dy, int64_t lddy, const float* __restrict__ a, int64_t lda,
-                                                 int rows, int N, float* __restrict__ dp, int64_t ldp) {
-  const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * 4;
-  if (n >= ldp) return;
-  for (int64_t r = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.y * 4) {
-    Vec16<float> t = load16_part(dy + r * lddy + n, N - n);
-    if (a) {
-      const Vec16<float> x = load16_part(a + r * lda + n, N - n);
+// Copies of operands in the workspace: rows of ldd elements with zeros behind the cols-th,
+// and with a gate only the elements where that is above 0 (dP; NaN is not).
+template <typename T>
+struct PadJob {
+  const T *src, *gate;
+  int64_t ld, ldgate, ldd;
+  int rows, cols;
+  T* dst;
+};
+template <typename T>
+struct PadJobs {
+  PadJob<T> job[3];
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_fc_pad(PadJobs<T> jobs) {
+  constexpr int V = Vec16<T>::N;
+  const PadJob<T>& j = jobs.job[blockIdx.z];
+  const int n = (blockIdx.x * 64 + (threadIdx.x & 63)) * V;
+  if (n >= j.ldd) return;
+  for (int64_t r = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6); r < j.rows; r += (int64_t)gridDim.y * 4) {
+    Vec16<T> t = load16_part(j.src + r * j.ld + n, j.cols - n);
+    if (j.gate) {
+      const Vec16<T> x = load16_part(j.gate + r * j.ldgate + n, j.cols - n);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t.v[e] = x.v[e] > 0.f ? t.v[e] : 0.f;
+      for (int e = 0; e < V; ++e) t.v[e] = to_f32(x.v[e]) > 0.f ? t.v[e] : (T)0.f;
     }
-    store16(dp + r * ldp + n, t);
+    store16(j.dst + r * j.ldd + n, t);
   }
+}
+template <typename T>
+hipError_t launch_pad(const PadJobs<T>& jobs, int n, hipStream_t s) {
+  if (n == 0) return hipSuccess;
+  int64_t wide = 0, rows = 0;
+  for (int i = 0; i < n; ++i) {
+    wide = std::max(wide, jobs.job[i].ldd);
+    rows = std::max<int64_t>(rows, jobs.job[i].rows);
+  }
+  const unsigned cols = (unsigned)((wide + 64 * Vec16<T>::N - 1) / (64 * Vec16<T>::N));
+  const unsigned groups = (unsigned)std::max<int64_t>(1, std::min<int64_t>((rows + 3) / 4, std::max<int64_t>(64, 8192 / cols)));
+  hipLaunchKernelGGL((k_fc_pad<T>), dim3(cols, groups, n), dim3(256), 0, s, jobs);
+  return hipGetLastError();
 }
 
 template <typename T>
@@ -486,39 +552,35 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_fc_few(FewArgs<T> g) {
 
 // Direct loads: 16-byte granules, and a tile's rows within 32-bit offsets of its first.
 bool dma_ok(const bf16* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0 && ld < (1 << 23); }
-// The same where the granules run along `cols` columns: the last one is whole.
-bool dma_ok(const bf16* p, int64_t ld, int cols) { return dma_ok(p, ld) && cols % 8 == 0; }
 
-// Large tiles (256 x 256, 8 waves, one work-group a CU) read LDS less per product, where
-// they fill the chip.
+// Tiles of 256 x 256 (8 waves of 128 x 64, one work-group a CU) and 128 x 256 (4 of 64 x
+// 128) do more products a step and LDS byte than 128 x 128 (4 of 64 x 64), where they fill
+// the chip.  16,384 rows of 2,048 to 2,048: 118, 139 and 161 us; 52,000 of 256 to 1,024: -,
+// 44 and 50 us; of 1,024 to 256 (203 large tiles): -, 38 and 45 us.
 template <bool ATR, bool BTR>
 hipError_t launch_product(FcProduct g, bool aligned, hipStream_t s) {
+  int n = 0;
   auto tiles = [&](int bm, int bn) {
     g.mt = (g.M + bm - 1) / bm;
     g.nt = (g.N + bn - 1) / bn;
-    return (int64_t)g.mt * g.nt * g.splits;
+    n = (int)((int64_t)g.mt * g.nt * g.splits);
+    return n;
   };
-  if (!aligned || (g.gate && !dma_ok(g.gate, g.ldgate))) {
-    const dim3 grid((unsigned)tiles(128, 128)), block(256);
-    hipLaunchKernelGGL((k_fc_any<ATR, BTR>), grid, block, 0, s, g);
-    return hipGetLastError();
+  auto grid = [&](int most) { return dim3((unsigned)std::min(most, (n + kNumXcd - 1) / kNumXcd * kNumXcd)); };
+  if (!aligned) {
+    tiles(128, 128);
+    hipLaunchKernelGGL((k_fc_any<ATR, BTR>), dim3((unsigned)n), dim3(256), 0, s, g);
+  } else if (g.N % 8 != 0 || (uintptr_t)g.bias % 16 != 0) {
+    tiles(128, 128);
+    hipLaunchKernelGGL((k_fc_tile<ATR, BTR, true, 128, 128, 64, 64, 4>), grid(512), dim3(256), 0, s, g, n);
+  } else if (!ATR && g.K >= 512 && tiles(256, 256) >= 256) {
+    if constexpr (!ATR) hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 256, 256, 128, 64, 4>), grid(256), dim3(512), 0, s, g, n);
+  } else if (!ATR && tiles(128, 256) >= 256) {
+    if constexpr (!ATR) hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 128, 256, 64, 128, 3>), grid(512), dim3(256), 0, s, g, n);
+  } else {
+    tiles(128, 128);
+    hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 128, 128, 64, 64, 4>), grid(512), dim3(256), 0, s, g, n);
   }
-  if constexpr (!ATR) {
-    if (!g.gate && g.K >= 512 && tiles(256, 256) >= 256) {
-      const int n = (int)tiles(256, 256);
-      hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 256, 256, 128, 64, 4>), dim3(256), dim3(512), 0, s, g, n);
-      return hipGetLastError();
-    }
-  }
-  const int n = (int)tiles(128, 128);
-  const dim3 grid((unsigned)std::min(512, (n + kNumXcd - 1) / kNumXcd * kNumXcd)), block(256);
-  if constexpr (ATR || BTR) {
-    if (g.gate) {
-      hipLaunchKernelGGL((k_fc_tile<ATR, BTR, true, 128, 128, 64, 64, 3>), grid, block, 0, s, g, n);
-      return hipGetLastError();
-    }
-  }
-  hipLaunchKernelGGL((k_fc_tile<ATR, BTR, false, 128, 128, 64, 64, 4>), grid, block, 0, s, g, n);
   return hipGetLastError();
 }
 
@@ -593,41 +655,42 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
                        (const float*)nullptr, 0, mn, N, dw, db);
     return hipGetLastError();
   }
-  const T* gate = f.act == GDP_ACT_RELU ? act_out : nullptr;
+  // the operands, or their copies
+  int64_t lddy = f.ld_dy, ldx = f.ld_x, ldw = K;
+  PadJobs<T> jobs = {};
+  int n = 0;
+  auto copy = [&](const T*& src, int64_t& ld, const T* gate, int rows, int cols, int64_t ldd, size_t at) {
+    if (ldd == 0) return;
+    T* dst = reinterpret_cast<T*>(base + at);
+    jobs.job[n++] = {src, gate, ld, f.ld_act, ldd, rows, cols, dst};
+    src = dst;
+    ld = ldd;
+  };
+  copy(dy, lddy, f.act == GDP_ACT_RELU ? act_out : nullptr, M, N, p.ldp, p.dp);
+  if (dw || db) copy(x, ldx, nullptr, M, K, p.ldx, p.x);
+  if (dx) copy(w, ldw, nullptr, N, K, p.ldw, p.w);
+  hipError_t e = launch_pad(jobs, n, s);
+  if (e != hipSuccess) return e;
   if constexpr (sizeof(T) == 4) {
-    const T* dp = dy;
-    int64_t ldp = f.ld_dy;
-    hipError_t e = hipSuccess;
-    if (p.ldp > 0) {
-      float* t = reinterpret_cast<float*>(base + p.dp);
-      const dim3 grid((unsigned)(p.ldp / 4 + 63) / 64, (unsigned)std::min((M + 3) / 4, 4096));
-      hipLaunchKernelGGL(k_fc_mask, grid, dim3(256), 0, s, dy, f.ld_dy, gate, f.ld_act, M, N, t, p.ldp);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      dp = t;
-      ldp = p.ldp;
-    }
     if (dx) {
-      tr::GemmStrided<float, float> g = {dp, ldp, 1, w, K, 1, M, K, N, dx, f.ld_dx};
+      tr::GemmStrided<float, float> g = {dy, lddy, 1, w, ldw, 1, M, K, N, dx, f.ld_dx};
       g.res = dx_add;
       g.ldr = f.ld_dx_add;
       e = tr::launch_gemm_strided(g, nullptr, 0, s);
     }
     if (e != hipSuccess || (!dw && !db)) return e;
     float* out = dw ? dw : part + p.partial_floats;        // db alone: the product's place is scratch
-    tr::GemmStrided<float, float> g = {dp, 1, ldp, x, f.ld_x, 1, N, K, M, out, K};
+    tr::GemmStrided<float, float> g = {dy, 1, lddy, x, ldx, 1, N, K, M, out, K};
     g.rowsum = db;
     return tr::launch_gemm_strided(g, part, p.partial_floats, s);
   } else {
     FcProduct g = {};
     g.a = dy;
-    g.lda = f.ld_dy;
-    g.gate = gate;
-    g.ldgate = f.ld_act;
-    const bool rows_ok = dma_ok(dy, f.ld_dy);
+    g.lda = lddy;
     if (dx) {
       FcProduct d = g;
       d.b = w;
-      d.ldb = K;
+      d.ldb = ldw;
       d.M = M;
       d.N = K;
       d.K = d.k_per_split = N;
@@ -636,12 +699,12 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
       d.ldr = f.ld_dx_add;
       d.c = dx;
       d.ldc = f.ld_dx;
-      const hipError_t e = launch_product<false, true>(d, rows_ok && N % 8 == 0 && dma_ok(w, K, K), s);
+      e = launch_product<false, true>(d, dma_ok(dy, lddy) && dma_ok(w, ldw), s);
       if (e != hipSuccess) return e;
     }
     if (!dw && !db) return hipSuccess;
     g.b = x;
-    g.ldb = f.ld_x;
+    g.ldb = ldx;
     g.M = N;
     g.N = K;
     g.K = M;
@@ -649,7 +712,7 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
     g.k_per_split = p.rows_per_split;
     g.f = part;
     g.rowsum = part + p.splits * mn;
-    const hipError_t e = launch_product<true, true>(g, rows_ok && N % 8 == 0 && dma_ok(x, f.ld_x, K), s);
+    e = launch_product<true, true>(g, dma_ok(dy, lddy) && dma_ok(x, ldx), s);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_fc_join, dim3((unsigned)((mn + N + 255) / 256)), dim3(256), 0, s, (const float*)part,
                        (const float*)g.rowsum, p.splits, mn, N, dw, db);

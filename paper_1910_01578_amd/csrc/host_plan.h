@@ -131,8 +131,8 @@ constexpr int kFcFewRows = 64;      // rows up to which a FC layer deals k to a 
 int check_fc(const gdp_fc_layer* f);
 struct FcPlan {
   Carve c;
-  size_t dp, partial;
-  int64_t ldp;             // row stride of dP's copy in the workspace, 0: dy is used as it is
+  size_t dp, x, w, partial;
+  int64_t ldp, ldx, ldw;   // row strides of copies in the workspace, 0: the operand is used as it is
   int64_t partial_floats;  // fp32: the products' split sums
   int splits, rows_per_split;  // bf16: dW's pieces of rows
 };

@@ -71,6 +71,28 @@ __device__ __forceinline__ void dma16_lane(const void* p, const void* lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :: "v"((uint64_t)p), "s"(__builtin_amdgcn_readfirstlane(la)) : "memory", "m0");
 }
+// Several, i-th load i * 1024 bytes further in LDS; the instruction adds that constant to
+// the lanes' addresses too, so those (offsets or addresses) are given less i * 1024.  `lds`:
+// the LDS offset of the first load's granules (wave-uniform).
+__device__ __forceinline__ void dma16x2(gptr_t base, uint32_t v0, uint32_t v1, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
+               :: "v"(v0), "v"(v1), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
+__device__ __forceinline__ void dma16x4(gptr_t base, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+               "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+               :: "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
+__device__ __forceinline__ void dma16x2(const void* p0, const void* p1, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024"
+               :: "v"((uint64_t)p0), "v"((uint64_t)p1), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
+__device__ __forceinline__ void dma16x4(const void* p0, const void* p1, const void* p2, const void* p3, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024\n\t"
+               "global_load_lds_dwordx4 %2, off offset:2048\n\tglobal_load_lds_dwordx4 %3, off offset:3072"
+               :: "v"((uint64_t)p0), "v"((uint64_t)p1), "v"((uint64_t)p2), "v"((uint64_t)p3),
+                  "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // ROWS x COLS block of a row-major matrix (leading dimension ld; rows beyond
