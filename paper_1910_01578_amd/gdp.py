@@ -565,60 +565,59 @@ class RewardBaseline:
 # stream, or on `stream`, where outputs and workspaces are allocated too.
 # ----------------------------------------------------------------------------
 
+_t = _torch()
 _ACTS = {"none": 0, "relu": 1}
+_DTYPES = {_t.float32: GDP_F32, _t.bfloat16: GDP_BF16}
+# the current stream's handle without a Stream object around it (2.6 us a call less)
+_raw_stream = getattr(_t._C, "_cuda_getCurrentRawStream", None) or (lambda d: _t.cuda.current_stream(d).cuda_stream)
 
 
 def _bad(msg: str):
     raise GdpError(GDP_E_INVALID_ARG, msg)
 
 
-class _On:
-    """The tensor's GPU as the current device and, if given, a stream as its current one."""
-
-    def __init__(self, t, stream):
-        cuda = _torch().cuda
-        self.dev = None if t.device.index == cuda.current_device() else cuda.device(t.device)
-        self.st = None if stream is None else cuda.stream(stream)
-
-    def __enter__(self):
-        if self.dev is not None:
-            self.dev.__enter__()
-        if self.st is not None:
-            self.st.__enter__()
-        return int(_torch().cuda.current_stream().cuda_stream)
-
-    def __exit__(self, *e):
-        if self.st is not None:
-            self.st.__exit__(*e)
-        if self.dev is not None:
-            self.dev.__exit__(*e)
+def _placed(x, stream, call):
+    """call(the stream's handle) with x's GPU as the current one and `stream`, if given, as its current stream."""
+    d = x.get_device()
+    if stream is None and (d < 0 or d == _t.cuda.current_device()):
+        return call(_raw_stream(d) if d >= 0 else 0)
+    with _t.cuda.device(d), _t.cuda.stream(stream):
+        return call(_raw_stream(d))
 
 
 def _dtype_of(name, t) -> int:
-    torch = _torch()
-    if t.dtype is torch.bfloat16:
-        return GDP_BF16
-    if t.dtype is torch.float32:
-        return GDP_F32
-    _bad(f"{name} is {t.dtype}, not float32 or bfloat16")
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        _bad(f"{name} is {t.dtype}, not float32 or bfloat16")
+    return dt
 
 
 def _need(name, t, like, shape, dtype=None):
     """t has this shape, like's device, like's dtype (or the given one) and a contiguous last dimension."""
-    if t.device != like.device or t.device.type != "cuda":
+    dtype = dtype or like.dtype
+    d = like.get_device()
+    if t.shape == shape and t.dtype is dtype and t.get_device() == d >= 0 and t.is_contiguous():
+        return
+    if t.get_device() != d or d < 0:
         _bad(f"{name} is on {t.device}, not on {like.device}" if t.device != like.device else f"{name} is not on a GPU")
-    if t.dtype is not (dtype or like.dtype):
-        _bad(f"{name} is {t.dtype}, not {dtype or like.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype:
+        _bad(f"{name} is {t.dtype}, not {dtype}")
+    if t.shape != shape:
         _bad(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         _bad(f"{name}'s last dimension is not contiguous")
-    if len(shape) == 2 and 0 <= t.stride(0) < shape[1] and shape[0] > 1:
+    if len(shape) == 2 and shape[0] > 1 and t.stride(0) < shape[1]:
         _bad(f"{name}'s rows overlap")
 
 
+def _matrix(name, t):
+    if t.dim() != 2:
+        _bad(f"{name} is not a matrix")
+    return t.shape
+
+
 def _ld(t) -> int:
-    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
 
 
 def _dense(name, t):
@@ -626,118 +625,114 @@ def _dense(name, t):
         _bad(f"{name} is not contiguous")
 
 
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def layer_norm(x, gamma, beta, residual=None, eps: float = 1e-5, keep_sum: bool = False, stream=None):
     """LayerNorm of x (+ residual), [rows, width]; with keep_sum (y, sum), the sum being layer_norm_backward's h."""
-    torch = _torch()
     dt = _dtype_of("x", x)
-    if x.dim() != 2:
-        _bad("x is not a matrix")
-    rows, width = x.shape
-    _need("x", x, x, (rows, width))
+    rows, width = shape = _matrix("x", x)
+    _need("x", x, x, shape)
     _need("gamma", gamma, x, (width,))
     _need("beta", beta, x, (width,))
     if residual is not None:
-        _need("residual", residual, x, (rows, width))
-    with _On(x, stream) as st:
-        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-        s = torch.empty_like(y) if keep_sum else None
-        check(lib.gdp_layer_norm(rows, width, dt, x.data_ptr(), _ld(x), None if residual is None else residual.data_ptr(),
-                                 0 if residual is None else _ld(residual), gamma.data_ptr(), beta.data_ptr(), float(eps),
-                                 y.data_ptr(), width, None if s is None else s.data_ptr(), width, st))
-    return (y, s) if keep_sum else y
+        _need("residual", residual, x, shape)
+
+    def call(st):
+        y = _t.empty(shape, dtype=x.dtype, device=x.device)
+        s = _t.empty_like(y) if keep_sum else None
+        check(lib.gdp_layer_norm(rows, width, dt, x.data_ptr(), _ld(x), _ptr(residual),
+                                 0 if residual is None else _ld(residual), gamma.data_ptr(), beta.data_ptr(), eps,
+                                 y.data_ptr(), width, _ptr(s), width, st))
+        return (y, s) if keep_sum else y
+    return _placed(x, stream, call)
 
 
 def layer_norm_backward(h, gamma, dy, dsum=None, eps: float = 1e-5, stream=None):
     """The gradients of layer_norm at h (x, or the sum it kept): (dh, dgamma, dbeta), the last two fp32.  dsum: the
     gradient that reaches h past the LayerNorm, added to dh (the gradient of x and of residual)."""
-    torch = _torch()
     dt = _dtype_of("h", h)
-    if h.dim() != 2:
-        _bad("h is not a matrix")
-    rows, width = h.shape
-    _need("h", h, h, (rows, width))
+    rows, width = shape = _matrix("h", h)
+    _need("h", h, h, shape)
     _need("gamma", gamma, h, (width,))
-    _need("dy", dy, h, (rows, width))
+    _need("dy", dy, h, shape)
     if dsum is not None:
-        _need("dsum", dsum, h, (rows, width))
-    with _On(h, stream) as st:
-        dh = torch.empty((rows, width), dtype=h.dtype, device=h.device)
-        dg, db = (torch.empty(width, dtype=torch.float32, device=h.device) for _ in range(2))
+        _need("dsum", dsum, h, shape)
+
+    def call(st):
+        dh = _t.empty(shape, dtype=h.dtype, device=h.device)
+        dg = _t.empty(width, dtype=_t.float32, device=h.device)
+        db = _t.empty_like(dg)
         need = lib.gdp_layer_norm_workspace_bytes(rows, width)
         if need == 0:
-            _bad(last_error())
-        ws = torch.empty(need, dtype=torch.uint8, device=h.device)
-        check(lib.gdp_layer_norm_backward(rows, width, dt, h.data_ptr(), _ld(h), gamma.data_ptr(), float(eps),
-                                          dy.data_ptr(), _ld(dy), None if dsum is None else dsum.data_ptr(),
-                                          0 if dsum is None else _ld(dsum), dh.data_ptr(), width, dg.data_ptr(),
-                                          db.data_ptr(), ws.data_ptr(), need, st))
-    return dh, dg, db
+            raise GdpError(GDP_E_INVALID_ARG, last_error())
+        ws = _t.empty(need, dtype=_t.uint8, device=h.device)
+        check(lib.gdp_layer_norm_backward(rows, width, dt, h.data_ptr(), _ld(h), gamma.data_ptr(), eps, dy.data_ptr(),
+                                          _ld(dy), _ptr(dsum), 0 if dsum is None else _ld(dsum), dh.data_ptr(), width,
+                                          dg.data_ptr(), db.data_ptr(), ws.data_ptr(), need, st))
+        return dh, dg, db
+    return _placed(h, stream, call)
+
+
+def _fc_shapes(x, w, act):
+    dt = _dtype_of("x", x)
+    if act not in _ACTS:
+        _bad(f"act {act!r} is not one of {sorted(_ACTS)}")
+    rows, k = _matrix("x", x)
+    n = _matrix("w", w)[0]
+    _need("x", x, x, (rows, k))
+    _need("w", w, x, (n, k))
+    _dense("w", w)
+    return dt, rows, k, n
 
 
 def fc(x, w, b=None, act: str = "none", residual=None, keep_act: bool = False, stream=None):
     """act(x w^T + b) + residual for x [rows, K], w [N, K], act "none" or "relu"; with keep_act (y, a), a the
     activation's output before the residual, for fc_backward (without residual that is y)."""
-    torch = _torch()
-    dt = _dtype_of("x", x)
-    if act not in _ACTS:
-        _bad(f"act {act!r} is not one of {sorted(_ACTS)}")
-    if x.dim() != 2 or w.dim() != 2:
-        _bad("x and w are not both matrices")
-    rows, k = x.shape
-    n = w.shape[0]
-    _need("x", x, x, (rows, k))
-    _need("w", w, x, (n, k))
-    _dense("w", w)
+    dt, rows, k, n = _fc_shapes(x, w, act)
     if b is not None:
         _need("b", b, x, (n,))
     if residual is not None:
         _need("residual", residual, x, (rows, n))
-    with _On(x, stream) as st:
-        y = torch.empty((rows, n), dtype=x.dtype, device=x.device)
-        a = torch.empty_like(y) if keep_act else None
-        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), n, 0 if residual is None else _ld(residual), n, 0, 0)
-        check(lib.gdp_fc(ctypes.byref(f), x.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
-                         None if residual is None else residual.data_ptr(), y.data_ptr(),
-                         None if a is None else a.data_ptr(), st))
-    return (y, a) if keep_act else y
+
+    def call(st):
+        y = _t.empty((rows, n), dtype=x.dtype, device=x.device)
+        a = _t.empty_like(y) if keep_act else None
+        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), n, 0 if residual is None else _ld(residual), n)
+        check(lib.gdp_fc(ctypes.byref(f), x.data_ptr(), w.data_ptr(), _ptr(b), _ptr(residual), y.data_ptr(), _ptr(a), st))
+        return (y, a) if keep_act else y
+    return _placed(x, stream, call)
 
 
 def fc_backward(dy, x, w, act: str = "none", act_out=None, dx_add=None, need_dx: bool = True, stream=None):
     """The gradients of fc: (dx or None, dw, db), the last two fp32; act_out: the activation's output (with "relu");
     dx_add: what reaches x on another path, added to dx.  The residual's gradient is dy itself."""
-    torch = _torch()
-    dt = _dtype_of("x", x)
-    if act not in _ACTS:
-        _bad(f"act {act!r} is not one of {sorted(_ACTS)}")
-    if x.dim() != 2 or w.dim() != 2:
-        _bad("x and w are not both matrices")
-    rows, k = x.shape
-    n = w.shape[0]
-    _need("x", x, x, (rows, k))
+    dt, rows, k, n = _fc_shapes(x, w, act)
     _need("dy", dy, x, (rows, n))
-    _need("w", w, x, (n, k))
-    _dense("w", w)
     if act == "relu":
         if act_out is None:
             _bad("act_out is needed with relu")
         _need("act_out", act_out, x, (rows, n))
+    else:
+        act_out = None
     if dx_add is not None:
         _need("dx_add", dx_add, x, (rows, k))
-    with _On(x, stream) as st:
-        dx = torch.empty((rows, k), dtype=x.dtype, device=x.device) if need_dx else None
-        dw = torch.empty((n, k), dtype=torch.float32, device=x.device)
-        db = torch.empty(n, dtype=torch.float32, device=x.device)
-        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), 0, 0, _ld(act_out) if act == "relu" else 0, _ld(dy), k,
+
+    def call(st):
+        dx = _t.empty((rows, k), dtype=x.dtype, device=x.device) if need_dx else None
+        dw = _t.empty((n, k), dtype=_t.float32, device=x.device)
+        db = _t.empty(n, dtype=_t.float32, device=x.device)
+        f = GdpFcLayer(rows, k, n, dt, _ACTS[act], _ld(x), 0, 0, 0 if act_out is None else _ld(act_out), _ld(dy), k,
                        0 if dx_add is None else _ld(dx_add))
         need = lib.gdp_fc_workspace_bytes(ctypes.byref(f))
         if need == 0:
-            _bad(last_error())
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-        check(lib.gdp_fc_backward(ctypes.byref(f), dy.data_ptr(), x.data_ptr(), w.data_ptr(),
-                                  act_out.data_ptr() if act == "relu" else None,
-                                  None if dx_add is None else dx_add.data_ptr(), None if dx is None else dx.data_ptr(),
-                                  dw.data_ptr(), db.data_ptr(), ws.data_ptr(), need, st))
-    return dx, dw, db
+            raise GdpError(GDP_E_INVALID_ARG, last_error())
+        ws = _t.empty(need, dtype=_t.uint8, device=x.device)
+        check(lib.gdp_fc_backward(ctypes.byref(f), dy.data_ptr(), x.data_ptr(), w.data_ptr(), _ptr(act_out),
+                                  _ptr(dx_add), _ptr(dx), dw.data_ptr(), db.data_ptr(), ws.data_ptr(), need, st))
+        return dx, dw, db
+    return _placed(x, stream, call)
 
 
 def rel_bounds(n_buckets: int, reach: int):
@@ -788,81 +783,76 @@ class RelAttention:
         for n, w in (("ld_q", wq), ("ld_k", wk), ("ld_v", wk), ("ld_o", wq), ("ld_do", wq), ("ld_dq", wq),
                      ("ld_dk", wk), ("ld_dv", wk)):
             setattr(self._c, n, w)
-        self._ws = [lib.gdp_rel_attention_workspace_bytes(ctypes.byref(self._c), 0)]
-        if self._ws[0] == 0:
+        self._ws = lib.gdp_rel_attention_workspace_bytes(ctypes.byref(self._c), 0)   # the same for both types
+        if self._ws == 0:
             raise GdpError(GDP_E_INVALID_ARG, last_error())
 
     def _call(self, q, k, v, table, key_mask):
         """The arrays checked; a descriptor of this call's own."""
         wq, wk = self._widths
         dt = _dtype_of("q", q)
-        if k.dim() != 2 or k.shape[0] < self.n_rows:
+        rows = k.shape[0] if k.dim() == 2 else 0
+        if rows < self.n_rows:
             _bad(f"k has shape {tuple(k.shape)}, not at least {self.n_rows} rows of {wk}")
         _need("q", q, q, (self.n_queries, wq))
-        _need("k", k, q, (k.shape[0], wk))
-        _need("v", v, q, (k.shape[0], wk))
+        _need("k", k, q, (rows, wk))
+        _need("v", v, q, (rows, wk))
         _need("table", table, q, (self.heads, self.n_buckets))
         _dense("table", table)
         if key_mask is not None:
-            _need("key_mask", key_mask, q, (k.shape[0],), _torch().uint8)
+            _need("key_mask", key_mask, q, (rows,), _t.uint8)
         c = GdpRelAttn.from_buffer_copy(self._c)
         c.dtype, c.ld_q, c.ld_k, c.ld_v = dt, _ld(q), _ld(k), _ld(v)
         return c
 
-    def _workspace(self, c, backward):
-        # sizes differ with the type in the backward alone
-        need = lib.gdp_rel_attention_workspace_bytes(ctypes.byref(c), 1) if backward else self._ws[0]
-        if need == 0:
-            raise GdpError(GDP_E_INVALID_ARG, last_error())
-        return need
-
     def forward(self, q, k, v, table, key_mask=None, stream=None):
         """q [queries, heads * d_head]; k, v [rows, kv_heads * d_head]; table [heads, buckets]; key_mask [rows]
         uint8.  Returns (o like q, lse [queries, heads] fp32 in base 2, for backward)."""
-        torch = _torch()
         c = self._call(q, k, v, table, key_mask)
-        with _On(q, stream) as st:
-            o = torch.empty((self.n_queries, self._widths[0]), dtype=q.dtype, device=q.device)
-            lse = torch.empty((self.n_queries, self.heads), dtype=torch.float32, device=q.device)
-            need = self._workspace(c, False)
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+
+        def call(st):
+            o = _t.empty((self.n_queries, self._widths[0]), dtype=q.dtype, device=q.device)
+            lse = _t.empty((self.n_queries, self.heads), dtype=_t.float32, device=q.device)
+            ws = _t.empty(self._ws, dtype=_t.uint8, device=q.device)
             check(lib.gdp_rel_attention(ctypes.byref(c), q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
-                                        None if key_mask is None else key_mask.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                        ws.data_ptr(), need, st))
-        return o, lse
+                                        _ptr(key_mask), o.data_ptr(), lse.data_ptr(), ws.data_ptr(), self._ws, st))
+            return o, lse
+        return _placed(q, stream, call)
 
     def backward(self, dout, q, k, v, table, o, lse, key_mask=None, out=None, stream=None):
         """(dq, dk, dv, dtable) for dL/do, from the forward's inputs and results; dtable is fp32, rows of k and v
         that belong to no graph get zeros.  out: the arrays for dq, dk and dv (e.g. columns of one matrix), whose
         rows of no graph are left as they are."""
-        torch = _torch()
         c = self._call(q, k, v, table, key_mask)
         wq, wk = self._widths
         _need("dout", dout, q, (self.n_queries, wq))
         _need("o", o, q, (self.n_queries, wq))
-        _need("lse", lse, q, (self.n_queries, self.heads), torch.float32)
+        _need("lse", lse, q, (self.n_queries, self.heads), _t.float32)
         _dense("lse", lse)
         if out is not None:
-            for n, t, shape in zip(("dq", "dk", "dv"), out, (q.shape, k.shape, k.shape)):
-                _need(n, t, q, shape)
+            for n, t, like in zip(("dq", "dk", "dv"), out, (q, k, v)):
+                _need(n, t, q, like.shape)
         c.ld_do, c.ld_o = _ld(dout), _ld(o)
-        with _On(q, stream) as st:
+
+        def call(st):
             if out is None:
-                make = torch.empty if self.n_keys == k.shape[0] else torch.zeros
-                dq = torch.empty((self.n_queries, wq), dtype=q.dtype, device=q.device)
+                make = _t.empty if self.n_keys == k.shape[0] else _t.zeros
+                dq = _t.empty((self.n_queries, wq), dtype=q.dtype, device=q.device)
                 dk, dv = (make((k.shape[0], wk), dtype=q.dtype, device=q.device) for _ in range(2))
             else:
                 dq, dk, dv = out
                 c.ld_dq, c.ld_dk, c.ld_dv = _ld(dq), _ld(dk), _ld(dv)
-            dtable = torch.empty((self.heads, self.n_buckets), dtype=torch.float32, device=q.device)
-            need = self._workspace(c, True)
-            ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+            dtable = _t.empty((self.heads, self.n_buckets), dtype=_t.float32, device=q.device)
+            need = lib.gdp_rel_attention_workspace_bytes(ctypes.byref(c), 1)
+            if need == 0:
+                raise GdpError(GDP_E_INVALID_ARG, last_error())
+            ws = _t.empty(need, dtype=_t.uint8, device=q.device)
             check(lib.gdp_rel_attention_backward(ctypes.byref(c), dout.data_ptr(), q.data_ptr(), k.data_ptr(),
-                                                 v.data_ptr(), table.data_ptr(),
-                                                 None if key_mask is None else key_mask.data_ptr(), o.data_ptr(),
+                                                 v.data_ptr(), table.data_ptr(), _ptr(key_mask), o.data_ptr(),
                                                  lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
                                                  dtable.data_ptr(), ws.data_ptr(), need, st))
-        return dq, dk, dv, dtable
+            return dq, dk, dv, dtable
+        return _placed(q, stream, call)
 
 
 def debug_uniforms(seed: int, n: int, k: int, d: int, device="cuda", stream=None):

@@ -57,8 +57,7 @@ class RelPlacerLayer:
                                                  stream=stream)
         dh1, g["ln1_g"], g["ln1_b"] = gdp.layer_norm_backward(k["h1"], w["ln1_g"], dz, stream=stream)
         do, g["w_o"], g["b_o"] = gdp.fc_backward(dh1, k["o"], w["w_o"], stream=stream)
-        with gdp._On(k["x"], stream):
-            dqkv = gdp._torch().empty_like(k["qkv"])
+        dqkv = gdp._placed(k["x"], stream, lambda _: gdp._t.empty_like(k["qkv"]))
         *_, g["rel_table"] = self.attention.backward(do, *self._split(k["qkv"]), w["rel_table"], k["o"], k["lse"],
                                                      key_mask=k["key_mask"], out=self._split(dqkv), stream=stream)
         dx, g["w_qkv"], g["b_qkv"] = gdp.fc_backward(dqkv, k["x"], w["w_qkv"], dx_add=dh1, stream=stream)
