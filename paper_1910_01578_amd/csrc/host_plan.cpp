@@ -513,24 +513,21 @@ int check_rel(const gdp_rel_attn* a, bool backward) {
 void plan_rel(const gdp_rel_attn* a, bool backward, RelPlan* p) {
   carve_init(&p->c);
   int longest = 1;
-  int64_t wide = 0, wide_keys = 0;                 // blocks of 128
+  int64_t wide = 0;                                // blocks of 128 queries
   p->queries = 0;
   for (int g = 0; g < a->n_graphs; ++g) {
     longest = std::max(longest, a->len_h[g]);
     p->queries += rel_queries(a, g);
     wide += (rel_queries(a, g) + 127) / 128;
-    wide_keys += (a->len_h[g] + 127) / 128;
   }
   p->seg = std::min(a->seg_len, longest);
   p->mem = std::min(a->mem_len, longest);
   p->buckets = (a->n_bounds + 1) * (a->causal ? 1 : 2);
   // Two columns a wave halve the tile reads a product, where that leaves two work-groups
-  // a CU and the registers hold them (not three planes of d_h = 64, nor backward three
-  // planes or d_h = 64: they spill).
+  // a CU and the registers hold them (not three planes of d_h = 64).  The backward keeps one:
+  // with two, half as many waves fit (29,000 rows, d_h = 16: 110 and 155 us, so 92 and 147).
   const bool fits = a->dtype == GDP_BF16 || a->head_dim < 64;
   p->cols = fits && wide * a->n_heads >= 512 ? 2 : 1;
-  p->bwd_cols = a->dtype == GDP_BF16 && a->head_dim < 64 &&
-                        std::min(wide * a->n_heads, wide_keys * a->n_kv_heads) >= 512 ? 2 : 1;
   // Few queries: about two work-groups a CU in all, each at least 4 tiles of 64 keys.
   int most = 0;
   int64_t groups = 0;
@@ -543,7 +540,7 @@ void plan_rel(const gdp_rel_attn* a, bool backward, RelPlan* p) {
   if (!backward && most > 0 && most <= kRelFewQueries)
     p->parts = (int)std::max<int64_t>(1, std::min<int64_t>((512 + groups - 1) / groups, (seen + 255) / 256));
   p->key_blocks = 0;
-  for (int g = 0; g < a->n_graphs; ++g) p->key_blocks += (a->len_h[g] + 64 * p->bwd_cols - 1) / (64 * p->bwd_cols);
+  for (int g = 0; g < a->n_graphs; ++g) p->key_blocks += (a->len_h[g] + 63) / 64;
   p->d = carve_add(&p->c, backward ? (size_t)p->queries * a->n_heads * 4
                           : p->parts > 1 ? (size_t)p->queries * a->n_heads * p->parts * (a->head_dim + 4) * 4 : 256);
   p->table_partial = carve_add(&p->c, backward ? (size_t)p->key_blocks * a->n_heads * p->buckets * 4 : 0);

@@ -144,7 +144,7 @@ struct RelPlan {
   Carve c;
   int seg, mem;            // less where longer ones make no difference
   int buckets;
-  int cols, bwd_cols;      // 16-row columns a wave owns
+  int cols;                // 16-query columns a wave owns (forward; backward: one)
   int parts;               // forward with few queries: parts of the keys, each a work-group; else 0
   int64_t queries;         // rows of q
   int key_blocks;          // work-groups a head of the dK, dV kernel

@@ -44,6 +44,7 @@ namespace {
 constexpr int kTile = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescale = 8.0f;       // a row maximum is raised once scores pass it by 2^8
+constexpr float kLargest = 0x1p100f;   // of a row's sum whose maximum is not raised
 
 // What a kernel needs besides its arrays.
 struct Geo {
@@ -116,14 +117,27 @@ struct Tile {
   }
   Vec16<T> v[U][NP == 3 ? 2 : 1];
   static __device__ __forceinline__ int unit(int u) { return ((int)threadIdx.x + 256 * u) % (kTile * G); }
-  // rows [t0, t0 + 64) of src; rows at or past t1 copy row t1 - 1
-  __device__ __forceinline__ void load(const T* src, int64_t ld, int t0, int t1) {
+  // Where a work-group's tiles come from: rows [t0, t0 + 64), [t0 + 64, ..) of src, rows at or
+  // past t1 as copies of row t1 - 1; place is this thread's first element in a tile.
+  struct From {
+    const T* tile;                     // the next tile's first element (uniform)
+    int64_t ld;
+    int left;                          // rows from there on
+    int64_t place;
+    __device__ __forceinline__ From(const T* src, int64_t ld_, int t0, int t1)
+        : tile(src + (size_t)t0 * ld_), ld(ld_), left(t1 - t0), place(unit(0) / G * ld_ + unit(0) % G * 8) {}
+  };
+  __device__ __forceinline__ void load(From& f) {          // past the end: nothing that is used
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = min(t0 + unit(u) / G, t1 - 1);
-      const T* p = src + (size_t)r * ld + unit(u) % G * 8;
+      const T* p = f.tile + f.place + (int64_t)u * (256 / G) * f.ld;
+      if (f.left < kTile) p = f.tile + (int64_t)min(unit(u) / G, f.left - 1) * f.ld + unit(u) % G * 8;
 #pragma unroll
       for (int i = 0; i < (NP == 3 ? 2 : 1); ++i) v[u][i] = load16_any(p + i * Vec16<T>::N);
+    }
+    if (f.left > kTile) {
+      f.tile += kTile * f.ld;
+      f.left -= kTile;
     }
   }
   __device__ __forceinline__ void store(char* s) const {
@@ -192,7 +206,9 @@ struct Row {
   }
 };
 
-// acc[c] = tile rows [row0, row0 + 16) . the columns' rows
+// acc[c] = tile rows [row0, row0 + 16) . the columns' rows.  (What is added to them later,
+// the bias less the log-sum-exp, -D, is not made the instruction's addend: beside it the
+// products lose their low bits, dtable's error was 2.4e-6 instead of 4e-7.)
 template <typename T, int DH, int COLS>
 __device__ __forceinline__ void dot_rows(f32x4 (&acc)[COLS], const char* tile, int row0, const Row<T, DH> (&y)[COLS], int col,
                                          int g4) {
@@ -240,19 +256,24 @@ constexpr int buffers() { return planes<T>() == 3 && DH == 64 ? 1 : 2; }
 template <typename T, int DH>
 constexpr int tile_lds() { return buffers<T, DH>() * 2 * Tile<T, DH>::kBytes; }
 
-// Two arrays' tiles through LDS: load(x, y, i) takes tile i into registers, prep(i)
-// fills what else tile i needs in LDS (into buffer i & 1 of its own), work(x, y, i)
-// uses both.  Ends with a barrier, so that the caller may start again.
-template <typename T, int DH, typename Load, typename Prep, typename Work>
-__device__ __forceinline__ void for_tiles(char* lds, int tiles, Load load, Prep prep, Work work) {
+// Two arrays' tiles through LDS: from fx and fy, prep(i) fills what else tile i needs in
+// LDS (into buffer i & 1 of its own), work(x, y, i) uses both.  Ends with a barrier, so
+// that the caller may start again.
+template <typename T, int DH, typename Prep, typename Work>
+__device__ __forceinline__ void for_tiles(char* lds, int tiles, typename Tile<T, DH>::From fx, typename Tile<T, DH>::From fy,
+                                          Prep prep, Work work) {
   constexpr int NB = buffers<T, DH>(), kBuf = 2 * Tile<T, DH>::kBytes;
   Tile<T, DH> x, y;
-  load(x, y, 0);
+  auto load = [&]() {
+    x.load(fx);
+    y.load(fy);
+  };
+  load();
   prep(0);
   if constexpr (NB == 2) {
     x.store(lds);
     y.store(lds + Tile<T, DH>::kBytes);
-    load(x, y, min(1, tiles - 1));
+    load();
   }
   for (int i = 0; i < tiles; ++i) {
     __syncthreads();
@@ -261,17 +282,26 @@ __device__ __forceinline__ void for_tiles(char* lds, int tiles, Load load, Prep 
       char* nxt = lds + ((i + 1) & 1) * kBuf;
       x.store(nxt);
       y.store(nxt + Tile<T, DH>::kBytes);
-      load(x, y, min(i + 2, tiles - 1));
+      load();
     } else {
       x.store(cur);
       y.store(cur + Tile<T, DH>::kBytes);
-      load(x, y, min(i + 1, tiles - 1));
+      load();
       __syncthreads();
     }
     if (i + 1 < tiles) prep(i + 1);
     work(cur, cur + Tile<T, DH>::kBytes, i);
   }
   __syncthreads();
+}
+
+// f(whether a tile's pairs need masking, whether its biases are a diagonal's each), as constants
+template <typename F>
+__device__ __forceinline__ void by_tile(bool masked, bool diagonals, F f) {
+  if (!masked && !diagonals) f(std::false_type(), std::false_type());
+  else if (!masked) f(std::false_type(), std::true_type());
+  else if (!diagonals) f(std::true_type(), std::false_type());
+  else f(std::true_type(), std::true_type());
 }
 
 // Rows of a work block: graph g, queries (or keys) [i0, i0 + rows) of it.
@@ -397,19 +427,23 @@ __global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo 
     row[c] = (size_t)(rt.q0[b.g] + b.i0 + i);
     span[c] = span_of(e, p0 + i, len);
     qf[c].load(q + row[c] * e.ldq + head * DH, g4);
+  }
+  int common[2] = {0, 0};                                  // of tiles i and i + 1, by i & 1
+  uint64_t seen[2] = {~0ull, ~0ull};                       // their rows that the key mask admits
+  // CAREFUL: the maximum follows the scores.  Else a row keeps the maximum of the first
+  // tile that shows it a key; scores further above than fp32 reaches make its sum leave
+  // kLargest, and the work-group starts again.
+  auto pass = [&](auto careful) {
+  constexpr bool CAREFUL = decltype(careful)::value;
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) {
     m[c] = -INFINITY;
     lsum[c] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db][c] = zero4();
   }
-  int common[2] = {0, 0};                                  // of tiles i and i + 1, by i & 1
-  uint64_t seen[2] = {~0ull, ~0ull};                       // their rows that the key mask admits
   for_tiles<T, DH>(
-      lds, tiles,
-      [&](Tile<T, DH>& x, Tile<T, DH>& y, int i) {
-        x.load(kg, e.ldk, k0 + i * kTile, k1);
-        y.load(vg, e.ldv, k0 + i * kTile, k1);
-      },
+      lds, tiles, {kg, e.ldk, k0, k1}, {vg, e.ldv, k0, k1},
       [&](int i) {
         const int t0 = k0 + i * kTile;
         const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
@@ -465,34 +499,39 @@ __global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo 
                 if (!((on >> (kb * 16 + r)) & 1ull)) s[kb][c][r] = -INFINITY;
           }
         }
-        bool raise = false;
-        float top[COLS];
+        bool unset = false;
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) {
-          float t = -INFINITY;
-#pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) t = fmaxf(t, s[kb][c][r]);
-          t = fmaxf(t, xor_shfl(t, 16));
-          top[c] = fmaxf(t, xor_shfl(t, 32));
-          raise = raise || top[c] > (m[c] == -INFINITY ? -INFINITY : kRescale);
-        }
-        if (__any(raise)) {
+        for (int c = 0; c < COLS; ++c) unset = unset || m[c] == -INFINITY;
+        if (CAREFUL || __any(unset)) {
+          bool raise = false;
+          float top[COLS];
 #pragma unroll
           for (int c = 0; c < COLS; ++c) {
-            const bool up = top[c] > (m[c] == -INFINITY ? -INFINITY : kRescale);
-            const float by = up ? top[c] : 0.f, corr = !up ? 1.f : m[c] == -INFINITY ? 0.f : exp2_fast(-by);
-            if (up) m[c] = base[c] + by;
-            lsum[c] *= corr;
+            float t = -INFINITY;
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s[kb][c][r] -= by;
+              for (int r = 0; r < 4; ++r) t = fmaxf(t, s[kb][c][r]);
+            t = fmaxf(t, xor_shfl(t, 16));
+            top[c] = fmaxf(t, xor_shfl(t, 32));
+            raise = raise || top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
+          }
+          if (__any(raise)) {
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+            for (int c = 0; c < COLS; ++c) {
+              const bool up = top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
+              const float by = up ? top[c] : 0.f, corr = !up ? 1.f : m[c] == -INFINITY ? 0.f : exp2_fast(-by);
+              if (up) m[c] = base[c] + by;
+              lsum[c] *= corr;
 #pragma unroll
-              for (int r = 0; r < 4; ++r) oacc[db][c][r] *= corr;
+              for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[kb][c][r] -= by;
+#pragma unroll
+              for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) oacc[db][c][r] *= corr;
+            }
           }
         }
 #pragma unroll
@@ -526,6 +565,15 @@ __global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo 
   for (int c = 0; c < COLS; ++c) {
     lsum[c] += xor_shfl(lsum[c], 16);
     lsum[c] += xor_shfl(lsum[c], 32);
+  }
+  };
+  pass(std::false_type());
+  bool far = false;
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) far = far || !(lsum[c] < kLargest && finite_column(oacc, c));
+  if (__syncthreads_or(far)) pass(std::true_type());
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) {
     if ((wave * COLS + c) * 16 + col >= count) continue;
     if (!(lsum[c] * 0.f == 0.f) || !finite_column(oacc, c)) {
       const T* qr = q + row[c] * e.ldq + head * DH;
@@ -893,7 +941,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
   const Span first = span_of(e, p0, len), last = span_of(e, p0 + count - 1, len);
   const int k0 = first.lo, k1 = last.hi, tiles = (k1 - k0 + kTile - 1) / kTile;
 
-  Row<T, DH> qf[COLS], df[COLS];
+  Row<T, DH> qf[COLS];
+  Row<T, DH> df[COLS];
   constexpr bool REST = planes<T>() == 1;                  // an fp32 o leaves no rest
   f32x4 acc[DB][COLS], pk[DB][COLS];
   float L[COLS], D0[COLS], dsum[COLS];
@@ -921,11 +970,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
   int common[2] = {0, 0};
   uint64_t seen[2] = {~0ull, ~0ull};
   for_tiles<T, DH>(
-      lds, tiles,
-      [&](Tile<T, DH>& x, Tile<T, DH>& y, int i) {
-        x.load(kg, e.ldk, k0 + i * kTile, k1);
-        y.load(vg, e.ldv, k0 + i * kTile, k1);
-      },
+      lds, tiles, {kg, e.ldk, k0, k1}, {vg, e.ldv, k0, k1},
       [&](int i) {
         const int t0 = k0 + i * kTile;
         const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
@@ -944,10 +989,16 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
         const uint64_t admitted = i & 1 ? seen[1] : seen[0];
         const bool full = t0 >= last.lo && t0 + kTile <= first.hi && admitted == ~0ull;
         const float* d = diag.bias[i & 1] + (BQ - 1) - (wave * COLS * 16 + col) + 4 * g4;
-        const float bias = u >= 0 ? s_table[u] : 0.f;
+        by_tile(!full, u < 0, [&](auto masked, auto diagonals) {
+        constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
+        const float bias = DIAG ? 0.f : s_table[u];
         uint64_t on[COLS];
+        float less[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) on[c] = full ? ~0ull : (row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4);
+        for (int c = 0; c < COLS; ++c) {
+          on[c] = MASKED ? (row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4) : 0;
+          less[c] = bias - L[c];
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           float t[COLS][8], tp[COLS][8];
@@ -961,9 +1012,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
             for (int c = 0; c < COLS; ++c)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float add = u >= 0 ? bias : d[(kb - c) * 16 + r];
-                float p = exp2_fast(fmaf(s[c][r], e.sc, add - L[c])), g = dp[c][r];
-                if (!full && !((on[c] >> (kb * 16 + r)) & 1ull)) p = g = 0.f;
+                float p = exp2_fast(fmaf(s[c][r], e.sc, DIAG ? d[(kb - c) * 16 + r] - L[c] : less[c])), g = dp[c][r];
+                if (MASKED && !((on[c] >> (kb * 16 + r)) & 1ull)) p = g = 0.f;
                 dsum[c] = fmaf(p, g, dsum[c]);
                 t[c][4 * x + r] = p * (g - D0[c]);
                 tp[c][4 * x + r] = p;
@@ -986,6 +1036,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
             acc_rows<T, DH, COLS>(pk, sK, 32 * h, w, col, g4);
           }
         }
+        });
       });
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
@@ -1054,7 +1105,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
   __shared__ int16_t s_bucket[2][ND + 1];
   __shared__ __attribute__((aligned(16))) float s_l[2][kTile], s_d[2][kTile];
   __shared__ int s_lo[2][kTile], s_hi[2][kTile];
-  __shared__ float s_ds[4][32 * (KW + 1)];
+  constexpr int NG = 32 + KW - 1, DS = KW + 4;             // diagonals of 32 rows, their places in LDS
+  __shared__ __attribute__((aligned(16))) float s_ds[4][NG * DS];
   __shared__ float s_acc[4][NBK];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
   const int logical = xcd_remap(blockIdx.x, gridDim.x);
@@ -1066,6 +1118,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
   const uint8_t* mg = key_mask ? key_mask + kbase : nullptr;
   Buckets::stage(s_bounds, rb);
   for (int i = threadIdx.x; i < 4 * NBK; i += 256) s_acc[i / NBK][i % NBK] = 0.f;
+  for (int i = threadIdx.x; i < 4 * NG * DS; i += 256) s_ds[i / (NG * DS)][i % (NG * DS)] = 0.f;   // places outside the block stay 0
   __syncthreads();
   const Buckets bk(s_bounds, rb.n, e.causal);
   // queries that may see one of the keys: positions [pf, pl)
@@ -1073,7 +1126,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
   const int pl = min(len, (kf1 - 1 + e.mem) / e.seg * e.seg + e.seg);
   const int tiles = pl > pf ? (pl - pf + kTile - 1) / kTile : 0;
 
-  Row<T, DH> kf[COLS], vf[COLS];
+  Row<T, DH> kf[COLS];
+  Row<T, DH> vf[COLS];
   f32x4 ak[DB][COLS], av[DB][COLS];
   int key[COLS];
   bool live[COLS];
@@ -1103,12 +1157,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
     };
     if (tiles > 0)
       for_tiles<T, DH>(
-          lds, tiles,
-          [&](Tile<T, DH>& x, Tile<T, DH>& y, int i) {
-            const int i0 = pf - pos0 + i * kTile;
-            x.load(q + (size_t)q0 * e.ldq + head * DH, e.ldq, i0, pl - pos0);
-            y.load(dout + (size_t)q0 * e.lddo + head * DH, e.lddo, i0, pl - pos0);
-          },
+          lds, tiles, {q + (size_t)q0 * e.ldq + head * DH, e.ldq, pf - pos0, pl - pos0},
+          {dout + (size_t)q0 * e.lddo + head * DH, e.lddo, pf - pos0, pl - pos0},
           [&](int i) {
             const int t0 = pf + i * kTile, at = i & 1;
             const int u = bk.common(kf0 - (t0 + kTile - 1), kf0 + BK - 1 - t0);
@@ -1135,30 +1185,31 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
             const int t0 = pf + i * kTile, at = i & 1, u = at ? common[1] : common[0];
             const bool full = all && t0 + kTile <= pl && kf0 >= s_lo[at][kTile - 1] && kf1 <= s_hi[at][0];
             const float* d = diag.bias[at] + (kTile - 1) + wave * KW + col - 4 * g4;
-            const float bias = u >= 0 ? s_table[u] : 0.f;
             if (u >= 0 && u != cur) {
               flush();
               cur = u;
             }
+            by_tile(!full, u < 0, [&](auto masked, auto diagonals) {
+            constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
+            const float bias = DIAG ? 0.f : s_table[u];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float tp[COLS][8], ts[COLS][8];
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 const int row0 = 32 * h + 16 * x;
-                f32x4 s[COLS], dp[COLS];
-                dot_rows<T, DH, COLS>(s, sQ, row0, kf, col, g4);
-                dot_rows<T, DH, COLS>(dp, sD, row0, vf, col, g4);
                 const float4 l4 = *reinterpret_cast<const float4*>(&s_l[at][row0 + 4 * g4]);
                 const float4 d4 = *reinterpret_cast<const float4*>(&s_d[at][row0 + 4 * g4]);
                 const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
+                f32x4 s[COLS], dp[COLS];
+                dot_rows<T, DH, COLS>(s, sQ, row0, kf, col, g4);
+                dot_rows<T, DH, COLS>(dp, sD, row0, vf, col, g4);
 #pragma unroll
                 for (int c = 0; c < COLS; ++c)
 #pragma unroll
                   for (int r = 0; r < 4; ++r) {
-                    const float add = u >= 0 ? bias : d[16 * c - row0 - r];
-                    float p = exp2_fast(fmaf(s[c][r], e.sc, add - lr[r])), g = dp[c][r] - dr[r];
-                    if (!full) {
+                    float p = exp2_fast(fmaf(s[c][r], e.sc, (DIAG ? d[16 * c - row0 - r] : bias) - lr[r])), g = dp[c][r] - dr[r];
+                    if constexpr (MASKED) {
                       const int w = row0 + 4 * g4 + r;
                       if (!(live[c] && key[c] >= s_lo[at][w] && key[c] < s_hi[at][w])) p = g = 0.f;
                     }
@@ -1173,27 +1224,30 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
 #pragma unroll
               for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(ts[c]);
               acc_rows<T, DH, COLS>(ak, sQ, 32 * h, w, col, g4);
-              if (u >= 0) {
+              if constexpr (!DIAG) {
 #pragma unroll
                 for (int c = 0; c < COLS; ++c)
                   far += ((ts[c][0] + ts[c][1]) + (ts[c][2] + ts[c][3])) + ((ts[c][4] + ts[c][5]) + (ts[c][6] + ts[c][7]));
               } else {
-                float* m = s_ds[wave];
+                // diagonal key - row + 31, in it the key: a lane's own diagonal is a row of LDS
+                float* m = s_ds[wave] + (col - 4 * g4 + 31) * DS + col;
 #pragma unroll
                 for (int c = 0; c < COLS; ++c)
 #pragma unroll
                   for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) m[(16 * x + 4 * g4 + r) * (KW + 1) + 16 * c + col] = ts[c][4 * x + r];
+                    for (int r = 0; r < 4; ++r) m[(16 * c - 16 * x - r) * DS + 16 * c] = ts[c][4 * x + r];
                 wave_lds_sync();
                 const int shift = lane - 31;               // key - row of the lane's diagonal
-                float t = 0.f;
-#pragma unroll 8
-                for (int x = 0; x < KW; ++x) {
-                  const int y = x - shift;
-                  const float z = m[min(max(y, 0), 31) * (KW + 1) + x];
-                  t += y >= 0 && y < 32 ? z : 0.f;
+                f32x4 part = zero4();
+                const f32x4* mine = reinterpret_cast<const f32x4*>(s_ds[wave] + min(lane, NG - 1) * DS);
+#pragma unroll
+                for (int x = 0; x < KW / 4; ++x) {
+                  const f32x4 z = mine[x];
+#pragma unroll
+                  for (int r = 0; r < 4; ++r) part[r] += z[r];
                 }
+                float t = (part[0] + part[1]) + (part[2] + part[3]);
                 const int idx = wave * KW - 32 * h + shift + (kTile - 1);
                 int bu = -1;
                 if (idx >= 0 && idx < ND) bu = s_bucket[at][idx];
@@ -1209,6 +1263,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
                 wave_lds_sync();
               }
             }
+            });
           });
     flush();
     __syncthreads();
@@ -1383,7 +1438,7 @@ hipError_t launch_rel_attention_backward(const gdp_rel_attn& a, const RelPlan& p
   const RelBounds rb = bounds_of(a);
   float* D = reinterpret_cast<float*>(static_cast<char*>(ws) + p.d);
   float* partial = reinterpret_cast<float*>(static_cast<char*>(ws) + p.table_partial);
-  hipError_t err = by_shape<sizeof(T) == 2 ? 32 : 0>(a.head_dim, p.bwd_cols, [&](auto dh, auto cols) {
+  hipError_t err = by_shape<0>(a.head_dim, 1, [&](auto dh, auto cols) {
     const RelTable rq = table_of(a, 64 * cols, false), rk = table_of(a, 64 * cols, true);
     const int bq = rq.blk[rq.n], bkv = rk.blk[rk.n];
     if (bq > 0) {
