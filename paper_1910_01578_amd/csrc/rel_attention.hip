@@ -73,9 +73,11 @@ struct Buckets {
   const int* at;                       // LDS: the bounds, then INT_MAX up to 64
   int mine;                            // at[lane]
   __device__ __forceinline__ static void stage(int* lds, const RelBounds& b) {
-    if (threadIdx.x < 64) lds[threadIdx.x] = (int)threadIdx.x < b.n ? b.at[threadIdx.x] : INT32_MAX;
+    if (threadIdx.x < 64) lds[threadIdx.x] = bound(b, threadIdx.x);
   }
-  __device__ __forceinline__ Buckets(const int* lds, int n_, int causal_) : n(n_), causal(causal_), at(lds), mine(lds[threadIdx.x & 63]) {}
+  __device__ __forceinline__ static int bound(const RelBounds& b, int i) { return i < b.n ? b.at[i] : INT32_MAX; }
+  __device__ __forceinline__ Buckets(const int* lds, const RelBounds& b, int causal_)
+      : n(b.n), causal(causal_), at(lds), mine(bound(b, threadIdx.x & 63)) {}
   __device__ __forceinline__ int side(int rel) const { return rel > 0 && !causal ? n + 1 : 0; }
   // of one distance a lane
   __device__ __forceinline__ int of(int rel) const {
@@ -390,182 +392,201 @@ struct Diagonals {
 
 // Scores, forward ------------------------------------------------------------------------
 
+// Bound by vector instructions: a score takes one FMA, one exponential (a quarter of the
+// FMA's rate), one add to its row's sum and half a conversion.  A wave takes 32 of a tile's
+// keys at a time, scores to products with V: few registers hold scores, so a SIMD holds four
+// waves (d_h <= 32, bf16) whose matrix and vector work overlap.  52,000 queries, 8 heads of
+// 32, 1,024 keys a query: 136 us (with all 64 keys at once and two waves: 157); 26 us of it
+// do not depend on the number of keys (106 MB of arrays), each 64 keys cost 6.
 template <typename T, int DH, int COLS>
-__global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q,
-                                                 const T* __restrict__ k, const T* __restrict__ v,
-                                                 const T* __restrict__ table, const uint8_t* __restrict__ key_mask,
-                                                 T* __restrict__ o, float* __restrict__ lse) {
+constexpr int fwd_waves() { return planes<T>() == 1 && DH <= 32 ? 4 : 2; }
+
+template <typename T, int DH, int COLS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(fwd_waves<T, DH, COLS>())))
+void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+               const T* __restrict__ table, const uint8_t* __restrict__ key_mask, T* __restrict__ o, float* __restrict__ lse) {
   constexpr int DB = DH / 16, BQ = 64 * COLS, ND = kTile + BQ - 1;
   __shared__ __attribute__((aligned(16))) char lds[tile_lds<T, DH>()];
   __shared__ int s_bounds[64];
   __shared__ float s_table[2 * GDP_MAX_REL_BOUNDS + 2];
-  __shared__ Diagonals<ND + 1> diag;
+  __shared__ float s_diag[3][ND + 1];                      // a tile's biases by distance, tile i in buffer i % 3
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
   const int logical = xcd_remap(blockIdx.x, gridDim.x);
   const int head = logical % e.heads, kvh = head / e.share;
   const Block b = block_of(rt, logical / e.heads, BQ);
-  const int len = rt.len[b.g], nq = rt.q0[b.g + 1] - rt.q0[b.g], pos0 = len - nq;
-  const int count = min(BQ, nq - b.i0), p0 = pos0 + b.i0;
+  const int len = rt.len[b.g], nq = rt.q0[b.g + 1] - rt.q0[b.g];
+  const int count = min(BQ, nq - b.i0), p0 = len - nq + b.i0;
   const T* kg = k + (size_t)rt.start[b.g] * e.ldk + kvh * DH;
   const T* vg = v + (size_t)rt.start[b.g] * e.ldv + kvh * DH;
   const uint8_t* mg = key_mask ? key_mask + rt.start[b.g] : nullptr;
-  Buckets::stage(s_bounds, rb);
-  if ((int)threadIdx.x < e.buckets) s_table[threadIdx.x] = bias_of(table[(size_t)head * e.buckets + threadIdx.x]);
-  __syncthreads();
-  const Buckets bk(s_bounds, rb.n, e.causal);
+  const float bias = bias_of(table[(size_t)head * e.buckets + min((int)threadIdx.x, e.buckets - 1)]);
+  const Buckets bk(s_bounds, rb, e.causal);
   const Span first = span_of(e, p0, len), last = span_of(e, p0 + count - 1, len);
   const int k0 = first.lo, k1 = last.hi, tiles = (k1 - k0 + kTile - 1) / kTile;
+  auto query_of = [&](int c) { return (wave * COLS + c) * 16 + col; };
+  auto row_of = [&](int c) { return (size_t)(rt.q0[b.g] + b.i0 + min(query_of(c), count - 1)); };
 
   Row<T, DH> qf[COLS];
   f32x4 oacc[DB][COLS];
   float m[COLS], lsum[COLS];
   Span span[COLS];
-  size_t row[COLS];
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
-    const int i = min((wave * COLS + c) * 16 + col, count - 1);
-    row[c] = (size_t)(rt.q0[b.g] + b.i0 + i);
-    span[c] = span_of(e, p0 + i, len);
-    qf[c].load(q + row[c] * e.ldq + head * DH, g4);
+    span[c] = span_of(e, p0 + min(query_of(c), count - 1), len);
+    qf[c].load(q + row_of(c) * e.ldq + head * DH, g4);
   }
   int common[2] = {0, 0};                                  // of tiles i and i + 1, by i & 1
   uint64_t seen[2] = {~0ull, ~0ull};                       // their rows that the key mask admits
-  // CAREFUL: the maximum follows the scores.  Else a row keeps the maximum of the first
-  // tile that shows it a key; scores further above than fp32 reaches make its sum leave
-  // kLargest, and the work-group starts again.
-  auto pass = [&](auto careful) {
-  constexpr bool CAREFUL = decltype(careful)::value;
+  auto prep = [&](int i) {
+    if (i == 0) {                                          // the first tiles are on their way
+      Buckets::stage(s_bounds, rb);
+      if ((int)threadIdx.x < e.buckets) s_table[threadIdx.x] = bias;
+      __syncthreads();
+    }
+    const int t0 = k0 + i * kTile;
+    const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
+    if (u < 0 && (int)threadIdx.x < ND) s_diag[i % 3][threadIdx.x] = s_table[bk.of(t0 - (p0 + BQ - 1) + (int)threadIdx.x)];
+    const uint64_t s = mg ? __ballot(mg[min(t0 + lane, k1 - 1)] != 0) : ~0ull;
+    if (i & 1) {
+      common[1] = u;
+      seen[1] = s;
+    } else {
+      common[0] = u;
+      seen[0] = s;
+    }
+  };
+  // Tile i's products -> probabilities, their sums added up.  CAREFUL: the maximum follows
+  // the scores.  Else a row keeps the maximum of the first tile that shows it a key; scores
+  // further above than fp32 reaches make its sum leave kLargest, and the work-group starts
+  // again.
+  // 32 keys' products -> probabilities, their sums added up.  CAREFUL: the maximum follows
+  // the scores.  Else a row keeps the maximum of the first keys that it sees; scores further
+  // above than fp32 reaches make its sum leave kLargest, and the work-group starts again.
+  auto soften = [&](auto careful, f32x4 (&s)[2][COLS], int i, int h) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    const int t0 = k0 + i * kTile + 32 * h, u = i & 1 ? common[1] : common[0];
+    const uint32_t admitted = (uint32_t)((i & 1 ? seen[1] : seen[0]) >> (32 * h));
+    const bool full = t0 >= last.lo && t0 + 32 <= first.hi && admitted == ~0u;
+    float base[COLS];
 #pragma unroll
-  for (int c = 0; c < COLS; ++c) {
-    m[c] = -INFINITY;
-    lsum[c] = 0.f;
+    for (int c = 0; c < COLS; ++c) base[c] = m[c] == -INFINITY ? 0.f : m[c];
+    if (u >= 0) {
 #pragma unroll
-    for (int db = 0; db < DB; ++db) oacc[db][c] = zero4();
-  }
-  for_tiles<T, DH>(
-      lds, tiles, {kg, e.ldk, k0, k1}, {vg, e.ldv, k0, k1},
-      [&](int i) {
-        const int t0 = k0 + i * kTile;
-        const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
-        if (u < 0 && (int)threadIdx.x < ND) diag.bias[i & 1][threadIdx.x] = s_table[bk.of(t0 - (p0 + BQ - 1) + (int)threadIdx.x)];
-        const uint64_t s = mg ? __ballot(mg[min(t0 + lane, k1 - 1)] != 0) : ~0ull;
-        if (i & 1) {
-          common[1] = u;
-          seen[1] = s;
-        } else {
-          common[0] = u;
-          seen[0] = s;
-        }
-      },
-      [&](const char* sK, const char* sV, int i) {
-        const int t0 = k0 + i * kTile, u = i & 1 ? common[1] : common[0];
-        const uint64_t admitted = i & 1 ? seen[1] : seen[0];
-        const bool full = t0 >= last.lo && t0 + kTile <= first.hi && admitted == ~0ull;
-        f32x4 s[4][COLS];
+      for (int c = 0; c < COLS; ++c) {
+        const float add = s_table[u] - base[c];
 #pragma unroll
-        for (int kb = 0; kb < 4; ++kb) dot_rows<T, DH, COLS>(s[kb], sK, kb * 16, qf, col, g4);
-        float base[COLS];
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) base[c] = m[c] == -INFINITY ? 0.f : m[c];
-        if (u >= 0) {
-          const float bias = s_table[u];
+          for (int r = 0; r < 4; ++r) s[kb][c][r] = fmaf(s[kb][c][r], e.sc, add);
+      }
+    } else {
+      // column c is 16 queries later than c - 1, block kb 16 keys: one shift of both is one value
+      const float* d = s_diag[i % 3] + (BQ - 1) - (wave * COLS * 16 + col) + 4 * g4 + 32 * h;
+      float t[COLS + 1][4];
 #pragma unroll
-          for (int kb = 0; kb < 4; ++kb)
+      for (int w = 0; w <= COLS; ++w)
 #pragma unroll
-            for (int c = 0; c < COLS; ++c)
+        for (int r = 0; r < 4; ++r) t[w][r] = d[(w - COLS + 1) * 16 + r];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s[kb][c][r] = fmaf(s[kb][c][r], e.sc, bias - base[c]);
-        } else {
-          // column c is 16 queries later than c - 1, block kb 16 keys: one shift of both is one value
-          const float* d = diag.bias[i & 1] + (BQ - 1) - (wave * COLS * 16 + col) + 4 * g4;
+      for (int c = 0; c < COLS; ++c)
 #pragma unroll
-          for (int w = -(COLS - 1); w < 4; ++w)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float t = d[w * 16 + r];
+          for (int r = 0; r < 4; ++r) s[kb][c][r] = fmaf(s[kb][c][r], e.sc, t[kb - c + COLS - 1][r] - base[c]);
+    }
+    if (!full) {
 #pragma unroll
-              for (int c = 0; c < COLS; ++c)
-                if (w + c >= 0 && w + c < 4) s[w + c][c][r] = fmaf(s[w + c][c][r], e.sc, t - base[c]);
-            }
-        }
-        if (!full) {
+      for (int c = 0; c < COLS; ++c) {
+        const uint32_t on = ((uint32_t)row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4);
 #pragma unroll
-          for (int c = 0; c < COLS; ++c) {
-            const uint64_t on = (row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
+          for (int r = 0; r < 4; ++r)
+            s[kb][c][r] = (on >> (kb * 16 + r)) & 1u ? s[kb][c][r] : -INFINITY;
+      }
+    }
+    bool unset = false;
 #pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (!((on >> (kb * 16 + r)) & 1ull)) s[kb][c][r] = -INFINITY;
-          }
-        }
-        bool unset = false;
+    for (int c = 0; c < COLS; ++c) unset = unset || m[c] == -INFINITY;
+    if (CAREFUL || __any(unset)) {
+      bool raise = false;
+      float top[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) unset = unset || m[c] == -INFINITY;
-        if (CAREFUL || __any(unset)) {
-          bool raise = false;
-          float top[COLS];
+      for (int c = 0; c < COLS; ++c) {
+        float t = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < COLS; ++c) {
-            float t = -INFINITY;
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) t = fmaxf(t, s[kb][c][r]);
-            t = fmaxf(t, xor_shfl(t, 16));
-            top[c] = fmaxf(t, xor_shfl(t, 32));
-            raise = raise || top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
-          }
-          if (__any(raise)) {
-#pragma unroll
-            for (int c = 0; c < COLS; ++c) {
-              const bool up = top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
-              const float by = up ? top[c] : 0.f, corr = !up ? 1.f : m[c] == -INFINITY ? 0.f : exp2_fast(-by);
-              if (up) m[c] = base[c] + by;
-              lsum[c] *= corr;
-#pragma unroll
-              for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[kb][c][r] -= by;
-#pragma unroll
-              for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) oacc[db][c][r] *= corr;
-            }
-          }
-        }
+          for (int r = 0; r < 4; ++r) t = fmaxf(t, s[kb][c][r]);
+        t = fmaxf(t, xor_shfl(t, 16));
+        top[c] = fmaxf(t, xor_shfl(t, 32));
+        raise = raise || top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
+      }
+      if (__any(raise)) {
 #pragma unroll
         for (int c = 0; c < COLS; ++c) {
-          float sum[4];
+          const bool up = top[c] > (m[c] == -INFINITY ? -INFINITY : CAREFUL ? kRescale : INFINITY);
+          const float by = up ? top[c] : 0.f, corr = !up ? 1.f : m[c] == -INFINITY ? 0.f : exp2_fast(-by);
+          m[c] = up ? base[c] + by : m[c];
+          lsum[c] *= corr;
 #pragma unroll
-          for (int kb = 0; kb < 4; ++kb) {
+          for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[kb][c][r] = exp2_fast(s[kb][c][r]);
-            sum[kb] = (s[kb][c][0] + s[kb][c][1]) + (s[kb][c][2] + s[kb][c][3]);
-          }
-          lsum[c] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            for (int r = 0; r < 4; ++r) s[kb][c][r] -= by;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) oacc[db][c][r] *= corr;
         }
+      }
+    }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          Operand<planes<T>()> p[COLS];
+    for (int c = 0; c < COLS; ++c) {
+      float sum[2];
 #pragma unroll
-          for (int c = 0; c < COLS; ++c) {
-            float t[8];
+      for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              t[r] = s[2 * h][c][r];
-              t[4 + r] = s[2 * h + 1][c][r];
-            }
-            p[c] = operand_of<planes<T>()>(t);
+        for (int r = 0; r < 4; ++r) s[kb][c][r] = exp2_fast(s[kb][c][r]);
+        sum[kb] = (s[kb][c][0] + s[kb][c][1]) + (s[kb][c][2] + s[kb][c][3]);
+      }
+      lsum[c] += sum[0] + sum[1];
+    }
+  };
+  auto pass = [&](auto careful) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) {
+      m[c] = -INFINITY;
+      lsum[c] = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db][c] = zero4();
+    }
+    const typename Tile<T, DH>::From fk{kg, e.ldk, k0, k1}, fv{vg, e.ldv, k0, k1};
+    for_tiles<T, DH>(lds, tiles, fk, fv, prep, [&](const char* sK, const char* sV, int i) {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        f32x4 s[2][COLS];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) dot_rows<T, DH, COLS>(s[kb], sK, 32 * h + kb * 16, qf, col, g4);
+        soften(careful, s, i, h);
+        Operand<planes<T>()> p[COLS];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) {
+          float t[8];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            t[r] = s[0][c][r];
+            t[4 + r] = s[1][c][r];
           }
-          acc_rows<T, DH, COLS>(oacc, sV, 32 * h, p, col, g4);
+          p[c] = operand_of<planes<T>()>(t);
         }
-      });
+        acc_rows<T, DH, COLS>(oacc, sV, 32 * h, p, col, g4);
+      }
+    });
 #pragma unroll
-  for (int c = 0; c < COLS; ++c) {
-    lsum[c] += xor_shfl(lsum[c], 16);
-    lsum[c] += xor_shfl(lsum[c], 32);
-  }
+    for (int c = 0; c < COLS; ++c) {
+      lsum[c] += xor_shfl(lsum[c], 16);
+      lsum[c] += xor_shfl(lsum[c], 32);
+    }
   };
   pass(std::false_type());
   bool far = false;
@@ -574,10 +595,11 @@ __global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo 
   if (__syncthreads_or(far)) pass(std::true_type());
 #pragma unroll
   for (int c = 0; c < COLS; ++c) {
-    if ((wave * COLS + c) * 16 + col >= count) continue;
+    if (query_of(c) >= count) continue;
+    const size_t row = row_of(c);
     if (!(lsum[c] * 0.f == 0.f) || !finite_column(oacc, c)) {
-      const T* qr = q + row[c] * e.ldq + head * DH;
-      const int p = p0 + (wave * COLS + c) * 16 + col;
+      const T* qr = q + row * e.ldq + head * DH;
+      const int p = p0 + query_of(c);
       auto score = [&](int j) { return fmaf(dot_f32<T, DH>(qr, kg + (size_t)j * e.ldk), e.sc, s_table[bk.of(j - p)]); };
       f32x4 t[DB];
 #pragma unroll
@@ -601,9 +623,9 @@ __global__ __launch_bounds__(256) void k_rel_fwd(RelTable rt, RelBounds rb, Geo 
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
       const float t[4] = {oacc[db][c][0] * inv, oacc[db][c][1] * inv, oacc[db][c][2] * inv, oacc[db][c][3] * inv};
-      store4(o + row[c] * e.ldo + head * DH + db * 16 + 4 * g4, t);
+      store4(o + row * e.ldo + head * DH + db * 16 + 4 * g4, t);
     }
-    if (lse && g4 == 0) lse[row[c] * e.heads + head] = none ? -INFINITY : m[c] + log2f(lsum[c]);
+    if (lse && g4 == 0) lse[row * e.heads + head] = none ? -INFINITY : m[c] + log2f(lsum[c]);
   }
 }
 
@@ -724,7 +746,7 @@ __global__ __launch_bounds__(256) void k_rel_few(RelTable rt, RelBounds rb, Geo 
   for (int i = threadIdx.x; i < 16 * e.buckets; i += 256)
     s_table[i / e.buckets][i % e.buckets] = bias_of(table[(size_t)head_of(i / e.buckets) * e.buckets + i % e.buckets]);
   __syncthreads();
-  const Buckets bk(s_bounds, rb.n, e.causal);
+  const Buckets bk(s_bounds, rb, e.causal);
   const int pf = pos0 + query_of(0), pl = pos0 + query_of(15);
   const int k0 = span_of(e, pf, len).lo, k1 = span_of(e, pl, len).hi;
   const int tiles = (k1 - k0 + kTile - 1) / kTile, per = (tiles + parts - 1) / parts;
@@ -904,7 +926,7 @@ __global__ __launch_bounds__(256) void k_rel_join(RelTable rt, RelBounds rb, Geo
   for (int step = 64; step > 0; step >>= 1)
     if (g + step < rt.n && rt.q0[g + step] <= (int)row) g += step;
   const int len = rt.len[g], p = len - (rt.q0[g + 1] - rt.q0[g]) + (int)row - rt.q0[g];
-  const Buckets bk(s_bounds, rb.n, e.causal);
+  const Buckets bk(s_bounds, rb, e.causal);
   finish_few<T, DH, 1>(acc, M, L, dim, q + row * e.ldq + head * DH, k + (size_t)rt.start[g] * e.ldk + kvh * DH, e.ldk,
                        v + (size_t)rt.start[g] * e.ldv + kvh * DH, e.ldv, key_mask ? key_mask + rt.start[g] : nullptr,
                        span_of(e, p, len), p, e.sc, bk, table + (size_t)head * e.buckets, o + row * e.ldo + head * DH,
@@ -937,7 +959,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
   Buckets::stage(s_bounds, rb);
   if ((int)threadIdx.x < e.buckets) s_table[threadIdx.x] = bias_of(table[(size_t)head * e.buckets + threadIdx.x]);
   __syncthreads();
-  const Buckets bk(s_bounds, rb.n, e.causal);
+  const Buckets bk(s_bounds, rb, e.causal);
   const Span first = span_of(e, p0, len), last = span_of(e, p0 + count - 1, len);
   const int k0 = first.lo, k1 = last.hi, tiles = (k1 - k0 + kTile - 1) / kTile;
 
@@ -1120,7 +1142,7 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
   for (int i = threadIdx.x; i < 4 * NBK; i += 256) s_acc[i / NBK][i % NBK] = 0.f;
   for (int i = threadIdx.x; i < 4 * NG * DS; i += 256) s_ds[i / (NG * DS)][i % (NG * DS)] = 0.f;   // places outside the block stay 0
   __syncthreads();
-  const Buckets bk(s_bounds, rb.n, e.causal);
+  const Buckets bk(s_bounds, rb, e.causal);
   // queries that may see one of the keys: positions [pf, pl)
   const int pf = max(pos0, e.causal ? kf0 : kf0 / e.seg * e.seg);
   const int pl = min(len, (kf1 - 1 + e.mem) / e.seg * e.seg + e.seg);
