@@ -320,6 +320,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProdu
   aim(t_first);
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) fetch(s * kStage);
+  if constexpr (!F32 && !PART) dma::wait_vm_barrier<(NS - 1) * kLoads>();   // the first bias; a later one is older than a stage waited for
   for (int t = t_first; t < t_end; t += groups) {
     const TileAt<BM, BN> at(g, t);
     const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;

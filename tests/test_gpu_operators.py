@@ -457,6 +457,27 @@ def test_layer(dtype):
             assert _rel(t, ref_g[n]) <= tol, n
 
 
+@pytest.mark.parametrize("rows, k, n", [(211, 96, 160), (300, 256, 1024), (520, 512, 512)])
+def test_fc_bias_and_operands_from_cold_caches(rows, k, n):
+    """Nothing is read before it has arrived: every call's bias is new and no cache holds it."""
+    gdp = _gdp()
+    g = _gen(77)
+    x = _normal(g, rows, k, dtype=BF16)
+    w = _normal(g, n, k, dtype=BF16, scale=k ** -0.5)
+    xc, wc = x.cuda(), w.cuda()
+    flush = torch.empty(1 << 29, dtype=torch.uint8, device="cuda")
+    base = x.double() @ w.double().t()
+    for i in range(6):
+        b = _normal(g, n, dtype=BF16) * 8
+        bc = b.cuda()
+        flush.fill_(i)
+        y = gdp.fc(xc, wc, bc)
+        want = base + b.double()
+        # the output's rounding and fp32 sums of at most k + 1 terms
+        err = (y.cpu().double() - want).abs()
+        assert (err <= 2.0 ** -8 * want.abs() + (k + 1) * R.U * (x.double().abs() @ w.double().abs().t() + b.double().abs())).all()
+
+
 def _bits(ts):
     return [t.detach().contiguous().view(torch.uint8).cpu().numpy().tobytes() for t in ts]
 
