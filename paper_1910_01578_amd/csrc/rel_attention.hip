@@ -271,7 +271,7 @@ __device__ __forceinline__ void for_tiles(char* lds, int tiles, typename Tile<T,
     y.load(fy);
   };
   load();
-  prep(0);
+  auto now = prep(0);
   if constexpr (NB == 2) {
     x.store(lds);
     y.store(lds + Tile<T, DH>::kBytes);
@@ -291,11 +291,20 @@ __device__ __forceinline__ void for_tiles(char* lds, int tiles, typename Tile<T,
       load();
       __syncthreads();
     }
-    if (i + 1 < tiles) prep(i + 1);
-    work(cur, cur + Tile<T, DH>::kBytes, i);
+    auto next = now;
+    if (i + 1 < tiles) next = prep(i + 1);
+    work(cur, cur + Tile<T, DH>::kBytes, i, now);
+    now = next;
   }
   __syncthreads();
 }
+
+// What a tile's scores need to know of its keys: the bucket that holds all of them, or -1,
+// and those that the key mask admits.
+struct Keys {
+  int bucket;
+  uint64_t seen;
+};
 
 // f(whether a tile's pairs need masking, whether its biases are a diagonal's each), as constants
 template <typename F>
@@ -384,6 +393,16 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// A lane's value from N lanes on (before it) in its row of 16, 0 past the row's end.
+template <int N>
+__device__ __forceinline__ float row_left(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x100 + N, 0xf, 0xf, true));
+}
+template <int N>
+__device__ __forceinline__ float row_right(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x110 + N, 0xf, 0xf, true));
+}
+
 // The biases of a tile's diagonals: value i belongs to the distance first + i.
 template <int N>
 struct Diagonals {
@@ -435,8 +454,6 @@ void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q, const 
     span[c] = span_of(e, p0 + min(query_of(c), count - 1), len);
     qf[c].load(q + row_of(c) * e.ldq + head * DH, g4);
   }
-  int common[2] = {0, 0};                                  // of tiles i and i + 1, by i & 1
-  uint64_t seen[2] = {~0ull, ~0ull};                       // their rows that the key mask admits
   auto prep = [&](int i) {
     if (i == 0) {                                          // the first tiles are on their way
       Buckets::stage(s_bounds, rb);
@@ -447,13 +464,7 @@ void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q, const 
     const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
     if (u < 0 && (int)threadIdx.x < ND) s_diag[i % 3][threadIdx.x] = s_table[bk.of(t0 - (p0 + BQ - 1) + (int)threadIdx.x)];
     const uint64_t s = mg ? __ballot(mg[min(t0 + lane, k1 - 1)] != 0) : ~0ull;
-    if (i & 1) {
-      common[1] = u;
-      seen[1] = s;
-    } else {
-      common[0] = u;
-      seen[0] = s;
-    }
+    return Keys{u, s};
   };
   // Tile i's products -> probabilities, their sums added up.  CAREFUL: the maximum follows
   // the scores.  Else a row keeps the maximum of the first tile that shows it a key; scores
@@ -462,10 +473,10 @@ void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q, const 
   // 32 keys' products -> probabilities, their sums added up.  CAREFUL: the maximum follows
   // the scores.  Else a row keeps the maximum of the first keys that it sees; scores further
   // above than fp32 reaches make its sum leave kLargest, and the work-group starts again.
-  auto soften = [&](auto careful, f32x4 (&s)[2][COLS], int i, int h) {
+  auto soften = [&](auto careful, f32x4 (&s)[2][COLS], int i, int h, const Keys& keys) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    const int t0 = k0 + i * kTile + 32 * h, u = i & 1 ? common[1] : common[0];
-    const uint32_t admitted = (uint32_t)((i & 1 ? seen[1] : seen[0]) >> (32 * h));
+    const int t0 = k0 + i * kTile + 32 * h, u = keys.bucket;
+    const uint32_t admitted = (uint32_t)(keys.seen >> (32 * h));
     const bool full = t0 >= last.lo && t0 + 32 <= first.hi && admitted == ~0u;
     float base[COLS];
 #pragma unroll
@@ -561,13 +572,13 @@ void k_rel_fwd(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ q, const 
       for (int db = 0; db < DB; ++db) oacc[db][c] = zero4();
     }
     const typename Tile<T, DH>::From fk{kg, e.ldk, k0, k1}, fv{vg, e.ldv, k0, k1};
-    for_tiles<T, DH>(lds, tiles, fk, fv, prep, [&](const char* sK, const char* sV, int i) {
+    for_tiles<T, DH>(lds, tiles, fk, fv, prep, [&](const char* sK, const char* sV, int i, const Keys& keys) {
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
         f32x4 s[2][COLS];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) dot_rows<T, DH, COLS>(s[kb], sK, 32 * h + kb * 16, qf, col, g4);
-        soften(careful, s, i, h);
+        soften(careful, s, i, h, keys);
         Operand<planes<T>()> p[COLS];
 #pragma unroll
         for (int c = 0; c < COLS; ++c) {
@@ -989,8 +1000,6 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
 #pragma unroll
     for (int db = 0; db < DB; ++db) acc[db][c] = pk[db][c] = zero4();
   }
-  int common[2] = {0, 0};
-  uint64_t seen[2] = {~0ull, ~0ull};
   for_tiles<T, DH>(
       lds, tiles, {kg, e.ldk, k0, k1}, {vg, e.ldv, k0, k1},
       [&](int i) {
@@ -998,66 +1007,60 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
         const int u = bk.common(t0 - (p0 + BQ - 1), t0 + kTile - 1 - p0);
         if (u < 0 && (int)threadIdx.x < ND) diag.bias[i & 1][threadIdx.x] = s_table[bk.of(t0 - (p0 + BQ - 1) + (int)threadIdx.x)];
         const uint64_t s = mg ? __ballot(mg[min(t0 + lane, k1 - 1)] != 0) : ~0ull;
-        if (i & 1) {
-          common[1] = u;
-          seen[1] = s;
-        } else {
-          common[0] = u;
-          seen[0] = s;
-        }
+        return Keys{u, s};
       },
-      [&](const char* sK, const char* sV, int i) {
-        const int t0 = k0 + i * kTile, u = i & 1 ? common[1] : common[0];
-        const uint64_t admitted = i & 1 ? seen[1] : seen[0];
+      [&](const char* sK, const char* sV, int i, const Keys& keys) {
+        const int t0 = k0 + i * kTile, u = keys.bucket;
+        const uint64_t admitted = keys.seen;
         const bool full = t0 >= last.lo && t0 + kTile <= first.hi && admitted == ~0ull;
         const float* d = diag.bias[i & 1] + (BQ - 1) - (wave * COLS * 16 + col) + 4 * g4;
         by_tile(!full, u < 0, [&](auto masked, auto diagonals) {
-        constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
-        const float bias = DIAG ? 0.f : s_table[u];
-        uint64_t on[COLS];
-        float less[COLS];
+          constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
+          const float bias = DIAG ? 0.f : s_table[u];
+          uint64_t on[COLS];
+          float less[COLS];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c) {
-          on[c] = MASKED ? (row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4) : 0;
-          less[c] = bias - L[c];
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float t[COLS][8], tp[COLS][8];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int kb = 2 * h + x;
-            f32x4 s[COLS], dp[COLS];
-            dot_rows<T, DH, COLS>(s, sK, kb * 16, qf, col, g4);
-            dot_rows<T, DH, COLS>(dp, sV, kb * 16, df, col, g4);
-#pragma unroll
-            for (int c = 0; c < COLS; ++c)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                float p = exp2_fast(fmaf(s[c][r], e.sc, DIAG ? d[(kb - c) * 16 + r] - L[c] : less[c])), g = dp[c][r];
-                if (MASKED && !((on[c] >> (kb * 16 + r)) & 1ull)) p = g = 0.f;
-                dsum[c] = fmaf(p, g, dsum[c]);
-                t[c][4 * x + r] = p * (g - D0[c]);
-                tp[c][4 * x + r] = p;
-              }
+          for (int c = 0; c < COLS; ++c) {
+            on[c] = MASKED ? (row_bits(span[c].lo - t0, span[c].hi - t0) & admitted) >> (4 * g4) : 0;
+            less[c] = bias - L[c];
           }
-          Operand<planes<T>()> w[COLS];
 #pragma unroll
-          for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(t[c]);
-          acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
-          if constexpr (REST) {
+          for (int h = 0; h < 2; ++h) {
+            float t[COLS][8], tp[COLS][8];
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) {
+            for (int x = 0; x < 2; ++x) {
+              const int kb = 2 * h + x;
+              f32x4 s[COLS], dp[COLS];
+              dot_rows<T, DH, COLS>(s, sK, kb * 16, qf, col, g4);
+              dot_rows<T, DH, COLS>(dp, sV, kb * 16, df, col, g4);
 #pragma unroll
-              for (int r = 0; r < 8; ++r) t[c][r] -= to_f32(w[c].p[0][r]);
-              w[c] = operand_of<1>(t[c]);
+              for (int c = 0; c < COLS; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  float p = exp2_fast(fmaf(s[c][r], e.sc, DIAG ? d[(kb - c) * 16 + r] - L[c] : less[c])), g = dp[c][r];
+                  if (MASKED && !((on[c] >> (kb * 16 + r)) & 1ull)) p = g = 0.f;
+                  dsum[c] = fmaf(p, g, dsum[c]);
+                  t[c][4 * x + r] = p * (g - D0[c]);
+                  tp[c][4 * x + r] = p;
+                }
             }
-            acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
+            Operand<planes<T>()> w[COLS];
 #pragma unroll
-            for (int c = 0; c < COLS; ++c) w[c] = operand_of<1>(tp[c]);
-            acc_rows<T, DH, COLS>(pk, sK, 32 * h, w, col, g4);
+            for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(t[c]);
+            acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
+            if constexpr (REST) {
+#pragma unroll
+              for (int c = 0; c < COLS; ++c) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) t[c][r] -= to_f32(w[c].p[0][r]);
+                w[c] = operand_of<1>(t[c]);
+              }
+              acc_rows<T, DH, COLS>(acc, sK, 32 * h, w, col, g4);
+#pragma unroll
+              for (int c = 0; c < COLS; ++c) w[c] = operand_of<1>(tp[c]);
+              acc_rows<T, DH, COLS>(pk, sK, 32 * h, w, col, g4);
+            }
           }
-        }
         });
       });
 #pragma unroll
@@ -1105,31 +1108,45 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_q(RelTable rt, RelBounds rb,
   }
 }
 
+// x of the lane N before this one in its row of 16, if that lane's bucket is this one's
+template <int N>
+__device__ __forceinline__ float row_right_if(float x, int bucket) {
+  const int b = __builtin_amdgcn_update_dpp(-2, bucket, 0x110 + N, 0xf, 0xf, false);
+  const float t = row_right<N>(x);
+  return b == bucket ? t : 0.f;
+}
+
 // dK, dV and the table's gradient --------------------------------------------------------------
 
 // The work-group's keys against every query that sees one of them, head after head of
 // those that share the keys.  dtable: where a tile lies in one bucket its dS are added
-// up in a lane's register until the bucket changes; elsewhere a wave puts 32 rows of dS
-// into LDS, lane d adds up diagonal d, and a scan over lanes of one bucket adds those.
-// Per work-group and head the sums of the four waves go to partial in order.
+// up in a lane's register until the bucket changes.  Elsewhere sums go along diagonals: the
+// dS of row r of a block move r lanes within their 16 keys (a lane crossing keeps the value
+// for the next block), so that one register adds up a block's 16 rows of four, and each
+// wave and lane group leaves 80 sums a tile in LDS.  While the next tile is worked on, a
+// thread a distance adds up the 16 that belong to it, and a scan over 16 distances adds
+// those of one bucket.  Per work-group and head the sums go to partial in a fixed order.
+// 29,000 queries of 4 graphs, 8 heads of 16, 512 keys a query, most tiles on diagonals: 109 us,
+// the dQ pass 71; about half of it vector instructions, 14 a score.  (Diagonals through an LDS
+// transpose of every 32 rows and a scan of 64 lanes each: 129.)
 template <typename T, int DH, int COLS>
-__global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ dout,
-                                                    const T* __restrict__ q, const T* __restrict__ k,
-                                                    const T* __restrict__ v, const T* __restrict__ table,
-                                                    const uint8_t* __restrict__ key_mask,
-                                                    const float* __restrict__ lse, const float* __restrict__ D,
-                                                    T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ partial) {
-  constexpr int DB = DH / 16, BK = 64 * COLS, ND = kTile + BK - 1, KW = 16 * COLS, NBK = 2 * GDP_MAX_REL_BOUNDS + 2;
+__global__ __launch_bounds__(256, planes<T>() == 1 && DH <= 32 ? 3 : 2)
+void k_rel_bwd_kv(RelTable rt, RelBounds rb, Geo e, const T* __restrict__ dout, const T* __restrict__ q,
+                  const T* __restrict__ k, const T* __restrict__ v, const T* __restrict__ table,
+                  const uint8_t* __restrict__ key_mask, const float* __restrict__ lse, const float* __restrict__ D,
+                  T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ partial) {
+  static_assert(COLS == 1, "a wave's diagonals are those of 16 keys");
+  constexpr int DB = DH / 16, BK = 64, ND = kTile + BK - 1, KW = 16, NBK = 2 * GDP_MAX_REL_BOUNDS + 2;
+  constexpr int NG = kTile + KW;                           // a lane group's diagonals of a tile: key - row + 64 in [0, NG)
   __shared__ __attribute__((aligned(16))) char lds[tile_lds<T, DH>()];
   __shared__ int s_bounds[64];
   __shared__ float s_table[NBK];
   __shared__ Diagonals<ND + 1> diag;
-  __shared__ int16_t s_bucket[2][ND + 1];
   __shared__ __attribute__((aligned(16))) float s_l[2][kTile], s_d[2][kTile];
   __shared__ int s_lo[2][kTile], s_hi[2][kTile];
-  constexpr int NG = 32 + KW - 1, DS = KW + 4;             // diagonals of 32 rows, their places in LDS
-  __shared__ __attribute__((aligned(16))) float s_ds[4][NG * DS];
-  __shared__ float s_acc[4][NBK];
+  __shared__ float s_ds[2][16][NG];                        // by tile & 1, wave and lane group
+  __shared__ int8_t s_bucket[4][ND + 1];                   // of tile i's distances in i & 3
+  __shared__ float s_far[4][NBK], s_near[8][NBK];          // sums by bucket: of the waves' tiles; of rows of 16 distances
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
   const int logical = xcd_remap(blockIdx.x, gridDim.x);
   const int kv_heads = e.heads / e.share, kvh = logical % kv_heads, blk = logical / kv_heads;
@@ -1139,8 +1156,8 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
   const size_t kbase = (size_t)rt.start[b.g];
   const uint8_t* mg = key_mask ? key_mask + kbase : nullptr;
   Buckets::stage(s_bounds, rb);
-  for (int i = threadIdx.x; i < 4 * NBK; i += 256) s_acc[i / NBK][i % NBK] = 0.f;
-  for (int i = threadIdx.x; i < 4 * NG * DS; i += 256) s_ds[i / (NG * DS)][i % (NG * DS)] = 0.f;   // places outside the block stay 0
+  for (int i = threadIdx.x; i < 4 * NBK; i += 256) s_far[i / NBK][i % NBK] = 0.f;
+  for (int i = threadIdx.x; i < 8 * NBK; i += 256) s_near[i / NBK][i % NBK] = 0.f;
   __syncthreads();
   const Buckets bk(s_bounds, rb, e.causal);
   // queries that may see one of the keys: positions [pf, pl)
@@ -1169,131 +1186,137 @@ __global__ __launch_bounds__(256, 2) void k_rel_bwd_kv(RelTable rt, RelBounds rb
     const int head = kvh * e.share + sh;
     if ((int)threadIdx.x < e.buckets) s_table[threadIdx.x] = bias_of(table[(size_t)head * e.buckets + threadIdx.x]);
     __syncthreads();
-    int common[2] = {0, 0}, cur = -1;
+    int cur = -1, last = 0;                                // the buckets of far, and of the tile before
     float far = 0.f;
     auto flush = [&]() {
       const float t = wave_sum(far);
-      if (cur >= 0 && lane == 0) s_acc[wave][cur] += t;
+      if (cur >= 0 && lane == 0) s_far[wave][cur] += t;
       far = 0.f;
       wave_lds_sync();
     };
-    if (tiles > 0)
+    // wave 3's: lse and D of the next tile's row `lane`
+    float row_l = 0.f, row_d = 0.f;
+    auto load_row = [&](int i) {
+      const size_t r = (size_t)(q0 + min(pf + i * kTile + lane, pl - 1) - pos0) * e.heads + head;
+      row_l = lse[r];
+      row_d = D[r];
+    };
+    if (wave == 3 && tiles > 0) load_row(0);
+    auto collect = [&](int i) {                            // tile i's sums, all in LDS since a barrier: waves 2 and 3
+      if (last >= 0 || wave < 2) return;
+      int j = (int)threadIdx.x - 128;
+      asm volatile("" : "+v"(j));                          // else 16 addresses and masks live through the loop
+      const int bu = s_bucket[i & 3][j];
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int p = j + 1 - KW * w + 4 * g;
+          const float z = s_ds[i & 1][4 * w + g][min(max(p, 0), NG - 1)];
+          t += p >= 0 && p < NG ? z : 0.f;
+        }
+      // within a row of 16, the sum of a bucket's distances so far; its last one has all
+      t += row_right_if<1>(t, bu);
+      t += row_right_if<2>(t, bu);
+      t += row_right_if<4>(t, bu);
+      t += row_right_if<8>(t, bu);
+      const int nb = __builtin_amdgcn_update_dpp(-2, bu, 0x101, 0xf, 0xf, false);
+      if (bu >= 0 && nb != bu) s_near[j >> 4][bu] += t;
+    };
+    if (tiles > 0) {
       for_tiles<T, DH>(
           lds, tiles, {q + (size_t)q0 * e.ldq + head * DH, e.ldq, pf - pos0, pl - pos0},
           {dout + (size_t)q0 * e.lddo + head * DH, e.lddo, pf - pos0, pl - pos0},
           [&](int i) {
             const int t0 = pf + i * kTile, at = i & 1;
             const int u = bk.common(kf0 - (t0 + kTile - 1), kf0 + BK - 1 - t0);
-            if (u < 0 && (int)threadIdx.x < ND) {
-              const int rel = kf0 - (t0 + kTile - 1) + (int)threadIdx.x, bu = bk.of(rel);
-              diag.bias[at][threadIdx.x] = s_table[bu];
-              s_bucket[at][threadIdx.x] = (int16_t)(e.causal && rel > 0 ? -1 : bu);
+            if (u < 0 && wave < 2) {
+              const int j = threadIdx.x, rel = kf0 - (t0 + kTile - 1) + j, bu = bk.of(rel);
+              if (j < ND) diag.bias[at][j] = s_table[bu];
+              s_bucket[i & 3][j] = (int8_t)(j >= ND || (e.causal && rel > 0) ? -1 : bu);
             }
-            if (threadIdx.x >= 192) {                      // the wave that ND leaves idle most
+            if (wave == 3) {
               const int p = t0 + lane;
-              const bool ok = p < pl;
-              const size_t r = (size_t)(q0 + min(p, pl - 1) - pos0) * e.heads + head;
               const Span s = span_of(e, min(p, pl - 1), len);
-              const float l = lse[r];
-              s_l[at][lane] = l == -INFINITY ? INFINITY : l;
-              s_d[at][lane] = D[r];
-              s_lo[at][lane] = ok ? s.lo : INT32_MAX;
-              s_hi[at][lane] = ok ? s.hi : 0;
+              s_l[at][lane] = row_l == -INFINITY ? INFINITY : row_l;
+              s_d[at][lane] = row_d;
+              s_lo[at][lane] = p < pl ? s.lo : INT32_MAX;
+              s_hi[at][lane] = p < pl ? s.hi : 0;
+              load_row(i + 1);
             }
-            if (at) common[1] = u;
-            else common[0] = u;
+            return u;
           },
-          [&](const char* sQ, const char* sD, int i) {
-            const int t0 = pf + i * kTile, at = i & 1, u = at ? common[1] : common[0];
+          [&](const char* sQ, const char* sD, int i, int u) {
+            const int t0 = pf + i * kTile, at = i & 1;
+            if (i > 0) collect(i - 1);
+            last = u;
             const bool full = all && t0 + kTile <= pl && kf0 >= s_lo[at][kTile - 1] && kf1 <= s_hi[at][0];
             const float* d = diag.bias[at] + (kTile - 1) + wave * KW + col - 4 * g4;
             if (u >= 0 && u != cur) {
               flush();
               cur = u;
             }
+            float* const sums = s_ds[at][4 * wave + g4] + col;
             by_tile(!full, u < 0, [&](auto masked, auto diagonals) {
-            constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
-            const float bias = DIAG ? 0.f : s_table[u];
+              constexpr bool MASKED = decltype(masked)::value, DIAG = decltype(diagonals)::value;
+              const float bias = DIAG ? 0.f : s_table[u];
+              float next = 0.f;                            // of the 16 diagonals below the block's
+#pragma unroll planes<T>() == 1 ? 2 : 1
+              for (int h = 0; h < 2; ++h) {
+                float tp[8], ts[8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float tp[COLS][8], ts[COLS][8];
-#pragma unroll
-              for (int x = 0; x < 2; ++x) {
-                const int row0 = 32 * h + 16 * x;
-                const float4 l4 = *reinterpret_cast<const float4*>(&s_l[at][row0 + 4 * g4]);
-                const float4 d4 = *reinterpret_cast<const float4*>(&s_d[at][row0 + 4 * g4]);
-                const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
-                f32x4 s[COLS], dp[COLS];
-                dot_rows<T, DH, COLS>(s, sQ, row0, kf, col, g4);
-                dot_rows<T, DH, COLS>(dp, sD, row0, vf, col, g4);
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
+                for (int x = 0; x < 2; ++x) {
+                  const int row0 = 32 * h + 16 * x;
+                  const float4 l4 = *reinterpret_cast<const float4*>(&s_l[at][row0 + 4 * g4]);
+                  const float4 d4 = *reinterpret_cast<const float4*>(&s_d[at][row0 + 4 * g4]);
+                  const float lr[4] = {l4.x, l4.y, l4.z, l4.w}, dr[4] = {d4.x, d4.y, d4.z, d4.w};
+                  f32x4 s[1], dp[1];
+                  dot_rows<T, DH, 1>(s, sQ, row0, kf, col, g4);
+                  dot_rows<T, DH, 1>(dp, sD, row0, vf, col, g4);
 #pragma unroll
                   for (int r = 0; r < 4; ++r) {
-                    float p = exp2_fast(fmaf(s[c][r], e.sc, (DIAG ? d[16 * c - row0 - r] : bias) - lr[r])), g = dp[c][r] - dr[r];
+                    float p = exp2_fast(fmaf(s[0][r], e.sc, (DIAG ? d[-row0 - r] : bias) - lr[r])), g = dp[0][r] - dr[r];
                     if constexpr (MASKED) {
                       const int w = row0 + 4 * g4 + r;
-                      if (!(live[c] && key[c] >= s_lo[at][w] && key[c] < s_hi[at][w])) p = g = 0.f;
+                      const bool on = live[0] && key[0] >= s_lo[at][w] && key[0] < s_hi[at][w];
+                      p = on ? p : 0.f;
+                      g = on ? g : 0.f;
                     }
-                    tp[c][4 * x + r] = p;
-                    ts[c][4 * x + r] = p * g;
+                    tp[4 * x + r] = p;
+                    ts[4 * x + r] = p * g;
                   }
-              }
-              Operand<planes<T>()> w[COLS];
-#pragma unroll
-              for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(tp[c]);
-              acc_rows<T, DH, COLS>(av, sD, 32 * h, w, col, g4);
-#pragma unroll
-              for (int c = 0; c < COLS; ++c) w[c] = operand_of<planes<T>()>(ts[c]);
-              acc_rows<T, DH, COLS>(ak, sQ, 32 * h, w, col, g4);
-              if constexpr (!DIAG) {
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-                  far += ((ts[c][0] + ts[c][1]) + (ts[c][2] + ts[c][3])) + ((ts[c][4] + ts[c][5]) + (ts[c][6] + ts[c][7]));
-              } else {
-                // diagonal key - row + 31, in it the key: a lane's own diagonal is a row of LDS
-                float* m = s_ds[wave] + (col - 4 * g4 + 31) * DS + col;
-#pragma unroll
-                for (int c = 0; c < COLS; ++c)
-#pragma unroll
-                  for (int x = 0; x < 2; ++x)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) m[(16 * c - 16 * x - r) * DS + 16 * c] = ts[c][4 * x + r];
-                wave_lds_sync();
-                const int shift = lane - 31;               // key - row of the lane's diagonal
-                f32x4 part = zero4();
-                const f32x4* mine = reinterpret_cast<const f32x4*>(s_ds[wave] + min(lane, NG - 1) * DS);
-#pragma unroll
-                for (int x = 0; x < KW / 4; ++x) {
-                  const f32x4 z = mine[x];
-#pragma unroll
-                  for (int r = 0; r < 4; ++r) part[r] += z[r];
+                  if constexpr (DIAG) {
+                    const float* z = ts + 4 * x;
+                    sums[kTile - row0] = (next + z[0]) + (row_left<1>(z[1]) + (row_left<2>(z[2]) + row_left<3>(z[3])));
+                    next = row_right<15>(z[1]) + (row_right<14>(z[2]) + row_right<13>(z[3]));
+                  } else {
+                    far += (ts[4 * x] + ts[4 * x + 1]) + (ts[4 * x + 2] + ts[4 * x + 3]);
+                  }
                 }
-                float t = (part[0] + part[1]) + (part[2] + part[3]);
-                const int idx = wave * KW - 32 * h + shift + (kTile - 1);
-                int bu = -1;
-                if (idx >= 0 && idx < ND) bu = s_bucket[at][idx];
-                if (shift >= KW) bu = -1;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                  const float tv = __shfl_up(t, off);
-                  const int tb = __shfl_up(bu, off);
-                  if (lane >= off && tb == bu) t += tv;
-                }
-                const int nb = __shfl_down(bu, 1);
-                if (bu >= 0 && (lane == 63 || nb != bu)) s_acc[wave][bu] += t;
-                wave_lds_sync();
+                Operand<planes<T>()> w[1] = {operand_of<planes<T>()>(tp)};
+                acc_rows<T, DH, 1>(av, sD, 32 * h, w, col, g4);
+                w[0] = operand_of<planes<T>()>(ts);
+                acc_rows<T, DH, 1>(ak, sQ, 32 * h, w, col, g4);
               }
-            }
+              if constexpr (DIAG) sums[0] = next;
             });
           });
+      collect(tiles - 1);
+    }
     flush();
     __syncthreads();
     if ((int)threadIdx.x < e.buckets) {
       const int i = threadIdx.x;
-      partial[((size_t)blk * e.heads + head) * e.buckets + i] = (s_acc[0][i] + s_acc[1][i]) + (s_acc[2][i] + s_acc[3][i]);
+      float sum = (s_far[0][i] + s_far[1][i]) + (s_far[2][i] + s_far[3][i]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) s_acc[w][i] = 0.f;
+      for (int w = 0; w < 4; ++w) s_far[w][i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        sum += s_near[w][i];
+        s_near[w][i] = 0.f;
+      }
+      partial[((size_t)blk * e.heads + head) * e.buckets + i] = sum;
     }
     __syncthreads();
   }
