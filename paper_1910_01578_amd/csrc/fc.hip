@@ -4,7 +4,8 @@
 //   dP = dy where a > 0 (ReLU) or dy,  dx = dP W,  dW = dP^T x,  db = sum_rows dP
 //
 // fp32 goes through the update step's products (train_gemm.hip: three bf16 planes an
-// operand).  bf16 has two kernels here:
+// operand), or k_fc_any_f32 (the same planes, any width and alignment).  bf16 has two
+// kernels here:
 //   k_fc_tile  128 x 128 or 256 x 256 tiles, k in stages of 32 filled by direct loads.
 //              The operands stay in their memory order; one whose contraction dimension
 //              is not the fast one (W in dx, both in dW) is read by transposing LDS reads.
@@ -65,7 +66,8 @@ struct OpTile {
     } else {
       const int k = 8 * g4 + (col >> 2), c = r0 + 4 * (col & 3);
       const char* p = lds + (c % 8) * 2;
-      return join8(read_tr16(p + k * (R * 2) + (((c / 8) ^ key(k)) << 4)), read_tr16(p + (k + 4) * (R * 2) + (((c / 8) ^ key(k + 4)) << 4)));
+      return join8(read_tr16(p + k * (R * 2) + (((c / 8) ^ key(k)) << 4)),
+                   read_tr16(p + (k + 4) * (R * 2) + (((c / 8) ^ key(k + 4)) << 4)));
     }
   }
 };
@@ -134,8 +136,9 @@ struct Block {
           float v[8];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)acc[h + i][2 * jp][r]),
-                                                            __builtin_bit_cast(uint32_t, (float)acc[h + i][2 * jp + 1][r]), false, false);
+            const float lo = acc[h + i][2 * jp][r], hi = acc[h + i][2 * jp + 1][r];
+            const auto t = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi),
+                                                            false, false);
             const uint32_t own = t[0], other = t[1];       // (a bit cast of the element itself takes element 0)
             v[r] = __builtin_bit_cast(float, own);
             v[4 + r] = __builtin_bit_cast(float, other);
@@ -223,7 +226,8 @@ struct Feed {
     // past the edge: the last row (granule) again, its results are not stored
 #pragma unroll
     for (int i = 0; i < O::PER; ++i)
-      off[i] = (uint32_t)((TR ? O::row(i) * ld + min(O::gran(i) * 8, (rows - 1) & ~7) : min(O::row(i), rows - 1) * ld + O::gran(i) * 8) * 2) + kBack - i * 1024;
+      off[i] = (uint32_t)((TR ? O::row(i) * ld + min(O::gran(i) * 8, (rows - 1) & ~7)
+                              : min(O::row(i), rows - 1) * ld + O::gran(i) * 8) * 2) + kBack - i * 1024;
   }
   // the next stage to LDS address `to` (of this wave's first granule); left: k from there on
   __device__ __forceinline__ void fetch(uint32_t to, int left) {
@@ -282,7 +286,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProdu
     if constexpr (!F32 && !PART) {
       if (wave == 0 && lane < BN / 8) {                    // this tile's bias, older than its first stage
         const int n = t.n0 + lane * 8;
-        dma::dma16_lane(g.bias && n < g.N ? reinterpret_cast<const char*>(g.bias + n) : reinterpret_cast<const char*>(&kZeros), s_bias[parity]);
+        const void* from = g.bias && n < g.N ? static_cast<const void*>(g.bias + n) : &kZeros;
+        dma::dma16_lane(from, s_bias[parity]);
       }
       parity ^= 1;
     }
@@ -320,7 +325,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64, 2) void k_fc_tile(FcProdu
   aim(t_first);
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s) fetch(s * kStage);
-  if constexpr (!F32 && !PART) dma::wait_vm_barrier<(NS - 1) * kLoads>();   // the first bias; a later one is older than a stage waited for
+  // the first tile's bias is in (a later one is older than a stage waited for)
+  if constexpr (!F32 && !PART) dma::wait_vm_barrier<(NS - 1) * kLoads>();
   for (int t = t_first; t < t_end; t += groups) {
     const TileAt<BM, BN> at(g, t);
     const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
@@ -383,8 +389,9 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
     char* p = lds + (s & 1) * (TA::kBytes + TB::kBytes);
 #pragma unroll
     for (int i = 0; i < TA::PER; ++i) *reinterpret_cast<uint4*>(p + TA::pos(i) * 16) = *reinterpret_cast<const uint4*>(&va[i]);
+    p += TA::kBytes;
 #pragma unroll
-    for (int i = 0; i < TB::PER; ++i) *reinterpret_cast<uint4*>(p + TA::kBytes + TB::pos(i) * 16) = *reinterpret_cast<const uint4*>(&vb[i]);
+    for (int i = 0; i < TB::PER; ++i) *reinterpret_cast<uint4*>(p + TB::pos(i) * 16) = *reinterpret_cast<const uint4*>(&vb[i]);
   };
   const int steps = (at.K + kStep - 1) / kStep;
   const bool sums = F32 && g.rowsum && at.n0 == 0 && nw == 0;
@@ -405,6 +412,113 @@ __global__ __launch_bounds__(256, 2) void k_fc_any(FcProduct g) {
     for (int i = 0; i < 4; ++i) b.add(i, TA::frag(p, mw + 16 * i, col, g4), fb, sums);
   }
   b.template store<true>(g, at.m0 + mw, at.n0 + nw, at.z, col, g4, sums);
+}
+
+// fp32 of any alignment, both results from one product: 64 x 64 tiles, a wave 32 x 32 of
+// them, k in stages of 32 through registers into two LDS buffers, three bf16 planes each.
+template <typename T>
+struct FewArgs {
+  const T *x, *w, *bias, *res;
+  T *y, *act_out;
+  int64_t ldx, ldr, ldy, ldact;
+  int M, N, K, relu;
+};
+__global__ __launch_bounds__(256) void k_fc_any_f32(FewArgs<float> g) {
+  constexpr int BT = 64;
+  using O = OpTile<false, BT, 256>;
+  constexpr int kOperand = 3 * O::kBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[4 * kOperand];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
+  const int mw = (wave >> 1) * 32, nw = (wave & 1) * 32;
+  const int logical = xcd_remap(blockIdx.x, gridDim.x), nt = (g.N + BT - 1) / BT;
+  const int m0 = logical / nt * BT, n0 = logical % nt * BT;
+  const int k0 = O::gran(0) * 8;
+  const float* px = g.x + (int64_t)min(m0 + O::row(0), g.M - 1) * g.ldx;
+  const float* pw = g.w + (int64_t)min(n0 + O::row(0), g.N - 1) * g.K;
+  Vec16<float> vx[2], vw[2];
+  auto load = [&](const float* p, int k, Vec16<float> (&v)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = k + 4 * i;
+      if (at < g.K) v[i] = load16_part(p + at, g.K - at);
+      else *reinterpret_cast<uint4*>(&v[i]) = make_uint4(0, 0, 0, 0);
+    }
+  };
+  auto fetch = [&](int s) {
+    load(px, s * kStep + k0, vx);
+    load(pw, s * kStep + k0, vw);
+  };
+  auto put_one = [&](char* to, const Vec16<float> (&v)[2]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[i] = v[0].v[i];
+      f[4 + i] = v[1].v[i];
+    }
+    const Operand<3> o = operand(f);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<bf16x8*>(to + q * O::kBytes + O::pos(0) * 16) = o.p[q];
+  };
+  auto put = [&](int s) {
+    char* p = lds + (s & 1) * (2 * kOperand);
+    put_one(p, vx);
+    put_one(p + kOperand, vw);
+  };
+  auto frag = [&](const char* p, int r0) {
+    Operand<3> o;
+#pragma unroll
+    for (int q = 0; q < 3; ++q) o.p[q] = O::frag(p + q * O::kBytes, r0, col, g4);
+    return o;
+  };
+  f32x4 top[2][2], low[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) top[i][j] = low[i][j] = zero4();
+  const int steps = (g.K + kStep - 1) / kStep;
+  fetch(0);
+  put(0);
+  if (steps > 1) fetch(1);
+  for (int s = 0; s < steps; ++s) {
+    __syncthreads();
+    if (s + 1 < steps) put(s + 1);
+    if (s + 2 < steps) fetch(s + 2);
+    const char* p = lds + (s & 1) * (2 * kOperand);
+    const Operand<3> b[2] = {frag(p + kOperand, nw), frag(p + kOperand, nw + 16)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Operand<3> a = frag(p, mw + 16 * i);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) mma_planes(b[j], a, top[i][j], low[i][j]);
+    }
+  }
+  const float least = g.relu ? 0.f : -INFINITY;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int n = n0 + nw + 16 * j + 4 * g4, left = g.N - n;
+    if (left <= 0) continue;
+    Vec16<float> bias = {};
+    if (g.bias) bias = load16_part(g.bias + n, left);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int m = m0 + mw + 16 * i + col;
+      if (m >= g.M) continue;
+      Vec16<float> v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        // an infinity's other planes are no part of its products: the first planes' sum says which
+        const float t = top[i][j][r], sum = t * 0.f == 0.f ? t + low[i][j][r] : t;
+        v.v[r] = __builtin_elementwise_maximum(sum + bias.v[r], least);      // NaN stays
+      }
+      if (g.act_out) store16_part(g.act_out + (int64_t)m * g.ldact + n, v, left);
+      if (g.res) {
+        const Vec16<float> t = load16_part(g.res + (int64_t)m * g.ldr + n, left);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v.v[r] += t.v[r];
+      }
+      store16_part(g.y + (int64_t)m * g.ldy + n, v, left);
+    }
+  }
 }
 
 // The splits' sums in order, in double.  entries of dW, then of db.
@@ -490,14 +604,6 @@ __device__ __forceinline__ f32x4 few_mma(const Vec16<T>& a, const Vec16<T>& b, f
   }
   return c;
 }
-
-template <typename T>
-struct FewArgs {
-  const T *x, *w, *bias, *res;
-  T *y, *act_out;
-  int64_t ldx, ldr, ldy, ldact;
-  int M, N, K, relu;
-};
 
 constexpr int kFewWaves = 8;
 template <typename T, int MB>
@@ -601,6 +707,17 @@ hipError_t launch_fc(const gdp_fc_layer& f, const T* x, const T* w, const T* b, 
     return hipGetLastError();
   }
   if constexpr (sizeof(T) == 4) {
+    // the update step's product loads and stores whole vectors and takes k in whole stages;
+    // element by element it is the slower one (relu of 2,503 rows of 131 to 517: 21 us there, 10
+    // here; 12,001 of 515 to 1,003: 213 and 101; 12,000 of 512 to 1,000, whole: 76 and 95)
+    auto whole = [](const void* p, int64_t ld) { return !p || (((uintptr_t)p & 15) == 0 && ld % 4 == 0); };
+    if (K % 32 != 0 || N % 4 != 0 || !whole(x, f.ld_x) || !whole(w, K) || !whole(y, f.ld_y) || !whole(residual, f.ld_res) ||
+        !whole(act_out, f.ld_act)) {
+      const FewArgs<T> g = {x, w, b, residual, y, act_out, f.ld_x, f.ld_res, f.ld_y, f.ld_act, M, N, K, relu};
+      const int64_t tiles = (int64_t)((M + 63) / 64) * ((N + 63) / 64);
+      hipLaunchKernelGGL(k_fc_any_f32, dim3((unsigned)tiles), dim3(256), 0, s, g);
+      return hipGetLastError();
+    }
     tr::GemmStrided<float, float> g = {x, f.ld_x, 1, w, 1, K, M, N, K, y, f.ld_y};
     g.bias_f = b;
     g.act = relu ? tr::ACT_GATE : tr::ACT_NONE;
@@ -723,7 +840,8 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
 
 #define GDP_FC_INST(T)                                                                                              \
   template hipError_t launch_fc<T>(const gdp_fc_layer&, const T*, const T*, const T*, const T*, T*, T*, hipStream_t); \
-  template hipError_t launch_fc_backward<T>(const gdp_fc_layer&, const FcPlan&, const T*, const T*, const T*, const T*, const T*, T*, \
+  template hipError_t launch_fc_backward<T>(const gdp_fc_layer&, const FcPlan&, const T*, const T*, const T*, const T*, \
+                                            const T*, T*, \
                                             float*, float*, void*, hipStream_t);
 GDP_FC_INST(float)
 GDP_FC_INST(bf16)
