@@ -838,11 +838,10 @@ hipError_t launch_fc_backward(const gdp_fc_layer& f, const FcPlan& p, const T* d
   }
 }
 
-#define GDP_FC_INST(T)                                                                                              \
+#define GDP_FC_INST(T)                                                                                                \
   template hipError_t launch_fc<T>(const gdp_fc_layer&, const T*, const T*, const T*, const T*, T*, T*, hipStream_t); \
-  template hipError_t launch_fc_backward<T>(const gdp_fc_layer&, const FcPlan&, const T*, const T*, const T*, const T*, \
-                                            const T*, T*, \
-                                            float*, float*, void*, hipStream_t);
+  template hipError_t launch_fc_backward<T>(const gdp_fc_layer&, const FcPlan&, const T*, const T*, const T*,         \
+                                            const T*, const T*, T*, float*, float*, void*, hipStream_t);
 GDP_FC_INST(float)
 GDP_FC_INST(bf16)
 #undef GDP_FC_INST
