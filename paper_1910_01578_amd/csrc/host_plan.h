@@ -122,12 +122,15 @@ void plan_sample(const gdp_graph* g, int32_t k_samples, SamplePlan* p);
 
 // ---- layer operators -----------------------------------------------------------
 // Row groups of LayerNorm's backward, each with one row of partial sums: enough to fill
-// the chip, of 4,096 elements at least, and their sums at most 2^20 floats a kind.
+// the chip, of 4,096 elements at least (4,096 rows of 256: 9.5 us, with 8,192 11.5, with
+// 16,384 16.8; 4,099 of 1,001: 24.6, 22.8 and 23.8), and their sums at most 2^20 floats a kind.
 int norm_backward_blocks(int64_t rows, int32_t width);
 int check_norm(int64_t rows, int32_t width, int32_t dtype, float eps);
 int check_ld(const char* name, int64_t ld, int64_t least);
 
-constexpr int kFcFewRows = 64;      // rows up to which a FC layer deals k to a work-group's waves
+// Rows up to which a FC layer deals k to a work-group's waves (bf16, 64 rows of 2,048 to
+// 2,048: 11.5 us, as tiles 21; of 256 to 1,024: 3.9 and 5.8; fp32 24 and 38, 5.4 and 7.9).
+constexpr int kFcFewRows = 64;
 int check_fc(const gdp_fc_layer* f);
 struct FcPlan {
   Carve c;
@@ -139,7 +142,10 @@ struct FcPlan {
 void plan_fc_backward(const gdp_fc_layer* f, FcPlan* p);
 
 int check_rel(const gdp_rel_attn* a, bool backward);
-constexpr int kRelFewQueries = 64;  // queries a graph up to which the keys are split over work-groups
+// Queries a graph up to which the keys are split over work-groups (bf16, 8 graphs of 12,000
+// keys, 8 heads of 64 on 2: 64 queries each 74 us, by the kernel for many 215, one query
+// 18 and 214; 1,000 keys: 19 and 24, 10 and 23).
+constexpr int kRelFewQueries = 64;
 struct RelPlan {
   Carve c;
   int seg, mem;            // less where longer ones make no difference

@@ -12,7 +12,10 @@
 // the groups of a work-group are added through LDS, and each work-group leaves one row of
 // partial sums; k_norm_weights adds those in a fixed order, in double.
 //
-// What bounds it: memory.
+// What bounds it: memory.  52,000 rows of 256, bf16: forward with a residual and the sum kept
+// 18 us (106 MB, 5.8 TB/s; what another kernel just wrote comes from the last cache), backward
+// 22.6 us and 3.8 for the weights' sums (4.0 TB/s in all); 4,099 rows of 1,001, which no
+// vector load fits: 9.3 and 24.6 us; 256 rows of 64, fp32: 3.6 us, a launch.
 #include <algorithm>
 
 #include "op_common.h"
@@ -209,7 +212,10 @@ __global__ __launch_bounds__(1024) void k_norm_weights(const float* __restrict__
   }
 }
 
-// The least group and vectors that hold a row: f(lanes, vectors a lane).
+// The least vectors a lane, then the least group, that hold a row: f(lanes, vectors a lane).
+// (52,000 rows of 256, 32 lanes of one vector against 16 of two: 18.5 and 19.1 us, backward
+// 25.1 and 30.1.  Above a wave's vectors two a lane come before a work-group's barriers, 64 of
+// two against 256 of one at a width of 1,024: 85 and 92 us, backward 126 and 170.)
 template <typename T, typename F>
 hipError_t by_width(int width, F f) {
   using std::integral_constant;

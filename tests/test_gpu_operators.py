@@ -457,6 +457,20 @@ def test_layer(dtype):
             assert _rel(t, ref_g[n]) <= tol, n
 
 
+@pytest.mark.parametrize("rows, k, n", [(50, 40, 24), (200, 41, 23), (200, 64, 64)])
+def test_fc_largest_values(rows, k, n):
+    """fp32 values that no bf16 holds, with products that fp32 holds."""
+    gdp = _gdp()
+    g = _gen(78)
+    x, w = _normal(g, rows, k), _normal(g, n, k)
+    x[::3, 5] = 3.4028e38
+    w[:, 5] = _normal(g, n, scale=1e-3).clamp(-0.25, 0.25)
+    y = gdp.fc(x.cuda(), w.cuda()).cpu().double()
+    big = x.double().abs() @ w.double().abs().t()
+    assert torch.isfinite(y).all()
+    assert ((y - x.double() @ w.double().t()).abs() <= (k + 1) * R.U * big).all()
+
+
 @pytest.mark.parametrize("rows, k, n", [(211, 96, 160), (300, 256, 1024), (520, 512, 512)])
 def test_fc_bias_and_operands_from_cold_caches(rows, k, n):
     """Nothing is read before it has arrived: every call's bias is new and no cache holds it."""
