@@ -2,6 +2,7 @@
 float64, at sizes and masks where they can go wrong; bounds in operator_refs.py."""
 import ctypes
 import math
+import threading
 
 import pytest
 import torch
@@ -246,6 +247,17 @@ def test_attention(name, dtype):
     _say("attention", name, dtype)
     ref, q, k, v, table, do = _attn_inputs(ATTNS[name], dtype, 11)
     _check_attn(ATTNS[name], dtype, q, k, v, table, do, pad=3, ref=ref)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("queries", ["every", "few"])
+def test_attention_most_graphs(queries, dtype):
+    """A batch of GDP_MAX_GRAPHS graphs, empty ones and ones without queries among them, the last one long."""
+    lengths = [(7 * i) % 11 for i in range(126)] + [0, 700]
+    nq = None if queries == "every" else [min(n, i % 3) for i, n in enumerate(lengths)]
+    case = _attn(lengths=lengths, queries=nq, heads=2, kv_heads=1, d_head=16, causal=True, bounds=[1, 2, 3, 300])
+    ref, q, k, v, table, do = _attn_inputs(case, dtype, 14)
+    _check_attn(case, dtype, q, k, v, table, do, ref=ref)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -528,6 +540,36 @@ def test_same_bits_again_and_on_other_streams(dtype):
             outs.append(run())
     torch.cuda.synchronize()
     assert all(_bits(o) == ref for o in outs)
+
+
+def test_calls_from_two_threads():
+    """Two host threads with streams of their own and one plan; errors belong to the thread that made them."""
+    run, _ = _all_calls(BF16)
+    ref = _bits(run())
+    torch.cuda.synchronize()
+    gdp = _gdp()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    out = run()
+                    if i == 0:
+                        with pytest.raises(gdp.GdpError, match="act"):
+                            gdp.fc(out[0], out[0], act="no such")
+            s.synchronize()
+            got[i] = _bits(out)
+        except BaseException as e:                         # what a thread raises is seen here
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not errors, errors
+    assert got == [ref, ref]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
