@@ -123,7 +123,8 @@ void plan_sample(const gdp_graph* g, int32_t k_samples, SamplePlan* p);
 // ---- layer operators -----------------------------------------------------------
 // Row groups of LayerNorm's backward, each with one row of partial sums: enough to fill
 // the chip, of 4,096 elements at least (4,096 rows of 256: 9.5 us, with 8,192 11.5, with
-// 16,384 16.8; 4,099 of 1,001: 24.6, 22.8 and 23.8), and their sums at most 2^20 floats a kind.
+// 16,384 16.8), and their sums at most 2^20 floats a kind (16,384 rows of 2,048: 89 us, with
+// 2^19 153).  The kernel may take fewer.
 int norm_backward_blocks(int64_t rows, int32_t width);
 int check_norm(int64_t rows, int32_t width, int32_t dtype, float eps);
 int check_ld(const char* name, int64_t ld, int64_t least);

@@ -15,7 +15,7 @@
 // What bounds it: memory.  52,000 rows of 256, bf16: forward with a residual and the sum kept
 // 18 us (106 MB, 5.8 TB/s; what another kernel just wrote comes from the last cache), backward
 // 22.6 us and 3.8 for the weights' sums (4.0 TB/s in all); 4,099 rows of 1,001, which no
-// vector load fits: 9.3 and 24.6 us; 256 rows of 64, fp32: 3.6 us, a launch.
+// vector load fits: 9.3 and 19.5 us; 256 rows of 64, fp32: 3.6 us, a launch.
 #include <algorithm>
 
 #include "op_common.h"
@@ -249,7 +249,11 @@ hipError_t launch_norm(const NormArgs<T>& a, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_norm_backward(const NormArgs<T>& a, float* partial, float* dgamma, float* dbeta, hipStream_t s) {
-  const int blocks = norm_backward_blocks(a.rows, a.width);
+  int blocks = norm_backward_blocks(a.rows, a.width);
+  // bf16 rows of two vectors a lane fill the registers of three work-groups a CU: two of them
+  // each, in one round (4,099 rows of 1,001: 24.9 us with 1,001 groups, 20.8 with 768, 19.5 so;
+  // 52,000 of 1,024: 124 and 120; fp32, whose vectors are half as long: 140 and 232)
+  if (sizeof(T) == 2 && a.width > 64 * Vec16<T>::N && a.width <= 128 * Vec16<T>::N) blocks = std::min(blocks, 512);
   if (blocks > 0) {
     const hipError_t e = by_width<T>(a.width, [&](auto lpr, auto c) {
       hipLaunchKernelGGL((k_norm_bwd<T, lpr, c>), dim3((unsigned)blocks), dim3(256), 0, s, a, partial);
