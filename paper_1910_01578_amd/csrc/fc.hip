@@ -10,8 +10,8 @@
 //              The operands stay in their memory order; one whose contraction dimension
 //              is not the fast one (W in dx, both in dW) is read by transposing LDS reads.
 //              (k_fc_any: the same through registers, for operands of odd alignment.)
-//   k_fc_few   up to 64 rows: 16 outputs a work-group, k dealt to its 8 waves, no LDS
-//              but for the waves' sums.  What bounds it: reading W.
+//   k_fc_few   few results: 16 outputs of up to 64 rows a work-group, k dealt to its 8
+//              waves, no LDS but for the waves' sums.  What bounds it: reading W.
 // Measured, bf16: 52,000 rows of 256 to 1,024 with ReLU 43 us (614 TFLOP/s; its 134 MB at the
 // rate of a copy, 27); 16,384 of 2,048 to 2,048 with a residual 118 to 135 us (1,020 to 1,160
 // TFLOP/s, as the clock holds); dX and dW of the former 41 and 42 us, dy's selection 49; one
@@ -621,11 +621,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_fc_few(FewArgs<T> g) {
   constexpr int KS = few_k<T>(), V = Vec16<T>::N, U = MB == 4 ? 2 : 4;
   __shared__ float part[kFewWaves][MB * 16][17];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g4 = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * (MB * 16);
   const T* w = g.w + (int64_t)min(n0 + col, g.N - 1) * g.K + g4 * V;
   const T* x[MB];
 #pragma unroll
-  for (int b = 0; b < MB; ++b) x[b] = g.x + (int64_t)min(16 * b + col, g.M - 1) * g.ldx + g4 * V;
+  for (int b = 0; b < MB; ++b) x[b] = g.x + (int64_t)min(m0 + 16 * b + col, g.M - 1) * g.ldx + g4 * V;
   f32x4 acc[MB];
 #pragma unroll
   for (int b = 0; b < MB; ++b) acc[b] = zero4();
@@ -654,11 +654,11 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_fc_few(FewArgs<T> g) {
     for (int r = 0; r < 4; ++r) part[wave][16 * b + col][4 * g4 + r] = acc[b][r];
   __syncthreads();
   for (int i = threadIdx.x; i < MB * 256; i += 64 * kFewWaves) {
-    const int m = i / 16, n = n0 + i % 16;
+    const int row = i / 16, m = m0 + row, n = n0 + i % 16;
     if (m >= g.M || n >= g.N) continue;
     float v = 0.f;
 #pragma unroll
-    for (int p = 0; p < kFewWaves; ++p) v += part[p][m][i % 16];
+    for (int p = 0; p < kFewWaves; ++p) v += part[p][row][i % 16];
     if (g.bias) v += to_f32(g.bias[n]);
     if (g.relu) v = v < 0.f ? 0.f : v;
     if (g.act_out) g.act_out[m * g.ldact + n] = from_f32<T>(v);
@@ -703,14 +703,24 @@ hipError_t launch_product(FcProduct g, bool aligned, hipStream_t s) {
 
 }  // namespace
 
+// Up to 16 rows, or while there are few 16 x 16 blocks of results, k is dealt to a
+// work-group's waves instead of walked by one tile's.  bf16, by blocks (of 64 rows a
+// work-group) and by tiles: 64 rows of 2,048 to 2,048 11.5 and 21 us, 256 rows (2,048
+// blocks) 20.7 and 21.8, 512 rows 38 and 22.5; 512 of 515 to 1,003 12.9 and 24.5; 64 of 256
+// to 1,024 3.9 and 5.8.  fp32: 128 rows of 2,048 to 2,048 (1,024 blocks) 24 and 39, 256 rows 45
+// and 39; 256 of 256 to 1,024 5.6 and 8.2, 1,024 rows 14.9 and 9.1.
+static bool few_rows(int M, int N, size_t bytes) {
+  return M <= 16 || (int64_t)((M + 15) / 16) * ((N + 15) / 16) <= (bytes == 2 ? 2048 : 1024);
+}
+
 template <typename T>
 hipError_t launch_fc(const gdp_fc_layer& f, const T* x, const T* w, const T* b, const T* residual, T* y, T* act_out,
                      hipStream_t s) {
   const int M = (int)f.rows, K = f.in_dim, N = f.out_dim, relu = f.act == GDP_ACT_RELU;
   if (M == 0) return hipSuccess;
-  if (M <= kFcFewRows) {
+  if (few_rows(M, N, sizeof(T))) {
     const FewArgs<T> g = {x, w, b, residual, y, act_out, f.ld_x, f.ld_res, f.ld_y, f.ld_act, M, N, K, relu};
-    const dim3 grid((unsigned)(N + 15) / 16), block(64 * kFewWaves);
+    const dim3 grid((unsigned)(N + 15) / 16, (unsigned)(M + 63) / 64), block(64 * kFewWaves);
     if (M <= 16) hipLaunchKernelGGL((k_fc_few<T, 1>), grid, block, 0, s, g);
     else if (M <= 32) hipLaunchKernelGGL((k_fc_few<T, 2>), grid, block, 0, s, g);
     else hipLaunchKernelGGL((k_fc_few<T, 4>), grid, block, 0, s, g);

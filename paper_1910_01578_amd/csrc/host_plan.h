@@ -129,9 +129,6 @@ int norm_backward_blocks(int64_t rows, int32_t width);
 int check_norm(int64_t rows, int32_t width, int32_t dtype, float eps);
 int check_ld(const char* name, int64_t ld, int64_t least);
 
-// Rows up to which a FC layer deals k to a work-group's waves (bf16, 64 rows of 2,048 to
-// 2,048: 11.5 us, as tiles 21; of 256 to 1,024: 3.9 and 5.8; fp32 24 and 38, 5.4 and 7.9).
-constexpr int kFcFewRows = 64;
 int check_fc(const gdp_fc_layer* f);
 struct FcPlan {
   Carve c;

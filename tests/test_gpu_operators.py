@@ -146,6 +146,26 @@ def test_fc(rows, k, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,n", [(1100, 96, 520), (1101, 97, 523), (2111, 72, 300), (4600, 40, 9), (40, 33, 17000),
+                                      (8192, 64, 1024), (16400, 512, 1030), (16384, 512, 1024)])
+def test_fc_many_results(rows, k, n, dtype):
+    """Every tile's kernel with its epilogues, at sizes where the few results' kernel does not stand in for it."""
+    gdp = _gdp()
+    _say("fc", rows, k, n, dtype)
+    g = _gen(rows + k + n)
+    x, w, b = _normal(g, rows, k, dtype=dtype), _normal(g, n, k, dtype=dtype, scale=k ** -0.5), _normal(g, n, dtype=dtype)
+    res = _normal(g, rows, n, dtype=dtype)
+    W, B, RES = w.cuda(), b.cuda(), res.cuda()
+    (y, by), (a, ba) = R.fc(x, w, b, "relu", res, dtype)
+    for pad in (0, 8, 5):
+        got, kept = gdp.fc(_rows(x, pad), W, B, act="relu", residual=_rows(res, pad), keep_act=True)
+        R.within(got, y, by, f"y {pad}")
+        R.within(kept, a, ba, f"a {pad}")
+        R.within(gdp.fc(_rows(x, pad), W, B, act="relu"), a, ba, f"a alone {pad}")
+        R.within(gdp.fc(_rows(x, pad), W, B, act="relu", residual=RES), y, by, f"y alone {pad}")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_fc_long_sum_over_rows(dtype):
     """dw and db over many rows: pieces of rows joined, no row lost or taken twice."""
     gdp = _gdp()
@@ -161,7 +181,7 @@ def test_fc_long_sum_over_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows", [7, 200])
+@pytest.mark.parametrize("rows", [7, 200, 9000])
 def test_fc_non_finite(rows, dtype):
     """NaN passes the activation; an infinity reaches its own row only."""
     gdp = _gdp()
@@ -469,7 +489,7 @@ def test_layer(dtype):
             assert _rel(t, ref_g[n]) <= tol, n
 
 
-@pytest.mark.parametrize("rows, k, n", [(50, 40, 24), (200, 41, 23), (200, 64, 64)])
+@pytest.mark.parametrize("rows, k, n", [(50, 40, 24), (200, 41, 23), (200, 64, 64), (3000, 41, 123), (3000, 64, 128)])
 def test_fc_largest_values(rows, k, n):
     """fp32 values that no bf16 holds, with products that fp32 holds."""
     gdp = _gdp()
@@ -483,7 +503,7 @@ def test_fc_largest_values(rows, k, n):
     assert ((y - x.double() @ w.double().t()).abs() <= (k + 1) * R.U * big).all()
 
 
-@pytest.mark.parametrize("rows, k, n", [(211, 96, 160), (300, 256, 1024), (520, 512, 512)])
+@pytest.mark.parametrize("rows, k, n", [(211, 96, 160), (300, 256, 1024), (2100, 96, 320), (1300, 256, 1024), (8192, 64, 1024)])
 def test_fc_bias_and_operands_from_cold_caches(rows, k, n):
     """Nothing is read before it has arrived: every call's bias is new and no cache holds it."""
     gdp = _gdp()
