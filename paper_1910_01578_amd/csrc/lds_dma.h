@@ -80,7 +80,7 @@ __device__ __forceinline__ void dma16x2(gptr_t base, uint32_t v0, uint32_t v1, u
 }
 __device__ __forceinline__ void dma16x4(gptr_t base, uint32_t v0, uint32_t v1, uint32_t v2, uint32_t v3, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-               "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+               "global_load_lds_dwordx4 %2, %4 offset:2*1024\n\tglobal_load_lds_dwordx4 %3, %4 offset:3*1024"
                :: "v"(v0), "v"(v1), "v"(v2), "v"(v3), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
 __device__ __forceinline__ void dma16x2(const void* p0, const void* p1, uint32_t lds) {
@@ -89,7 +89,7 @@ __device__ __forceinline__ void dma16x2(const void* p0, const void* p1, uint32_t
 }
 __device__ __forceinline__ void dma16x4(const void* p0, const void* p1, const void* p2, const void* p3, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024\n\t"
-               "global_load_lds_dwordx4 %2, off offset:2048\n\tglobal_load_lds_dwordx4 %3, off offset:3072"
+               "global_load_lds_dwordx4 %2, off offset:2*1024\n\tglobal_load_lds_dwordx4 %3, off offset:3*1024"
                :: "v"((uint64_t)p0), "v"((uint64_t)p1), "v"((uint64_t)p2), "v"((uint64_t)p3),
                   "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
