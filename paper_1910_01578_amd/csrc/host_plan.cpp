@@ -524,8 +524,10 @@ void plan_rel(const gdp_rel_attn* a, bool backward, RelPlan* p) {
   p->mem = std::min(a->mem_len, longest);
   p->buckets = (a->n_bounds + 1) * (a->causal ? 1 : 2);
   // Two columns a wave halve the tile reads a product, where that leaves two work-groups
-  // a CU and the registers hold them (not three planes of d_h = 64).  The backward keeps one:
-  // with two, half as many waves fit (29,000 rows, d_h = 16: 110 and 155 us, so 92 and 147).
+  // a CU and the registers hold them (not three planes of d_h = 64): 52,000 queries of 8 heads
+  // of 32, 147 us with two and 192 with one, 29,000 of 8 of 16 51 and 63.  The backward keeps
+  // one: with two, half as many waves fit (29,000 rows, d_h = 16: dK and dV 110 us with one and
+  // 155 with two, dQ 92 and 147).
   const bool fits = a->dtype == GDP_BF16 || a->head_dim < 64;
   p->cols = fits && wide * a->n_heads >= 512 ? 2 : 1;
   // Few queries: about two work-groups a CU in all, each at least 4 tiles of 64 keys.

@@ -415,7 +415,7 @@ struct Diagonals {
 // FMA's rate), one add to its row's sum and half a conversion.  A wave takes 32 of a tile's
 // keys at a time, scores to products with V: few registers hold scores, so a SIMD holds four
 // waves (d_h <= 32, bf16) whose matrix and vector work overlap.  52,000 queries, 8 heads of
-// 32, 1,024 keys a query: 136 us (with all 64 keys at once and two waves: 157); 26 us of it
+// 32, 1,024 keys a query: 133 us (with all 64 keys at once and two waves: 157); 26 us of it
 // do not depend on the number of keys (106 MB of arrays), each 64 keys cost 6.
 template <typename T, int DH, int COLS>
 constexpr int fwd_waves() { return planes<T>() == 1 && DH <= 32 ? 4 : 2; }
