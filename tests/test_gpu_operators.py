@@ -489,6 +489,32 @@ def test_layer(dtype):
             assert _rel(t, ref_g[n]) <= tol, n
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows, stride", [(60000, 40000), (60000, 40001), (60, 40000000)])
+def test_rows_far_apart(rows, stride, dtype):
+    """Row strides that put the last rows beyond 2^31 elements."""
+    gdp = _gdp()
+    if rows * stride * dtype.itemsize > torch.cuda.mem_get_info()[0] // 2:
+        pytest.skip("not enough memory")
+    g = _gen(41)
+    a, w, b = _normal(g, rows, 72, dtype=dtype), _normal(g, 72, 72, dtype=dtype, scale=0.1), _normal(g, 72, dtype=dtype)
+    room = torch.empty((rows - 1) * stride + 72, dtype=dtype, device="cuda")
+    x = room.as_strided((rows, 72), (stride, 1))
+    x.copy_(a)
+    W, B, A = w.cuda(), b.cuda(), a.cuda()
+    for far, near in ((gdp.layer_norm(x, B, B), gdp.layer_norm(A, B, B)),
+                      (gdp.layer_norm_backward(x, B, x), gdp.layer_norm_backward(A, B, A)),
+                      (gdp.fc(x, W, B, act="relu", residual=x), gdp.fc(A, W, B, act="relu", residual=A))):
+        for f, n in zip(far if isinstance(far, tuple) else (far,), near if isinstance(near, tuple) else (near,)):
+            if stride % 8 == 0:                            # the same kernels
+                assert torch.equal(f, n)
+            else:                                          # another order of sums: roundings differ by a step at most
+                assert _rel(f, n.double().cpu()) <= 2.0 ** -8
+    far = gdp.fc_backward(x, x, W, act="relu", act_out=x, dx_add=x)
+    for f, n in zip(far, gdp.fc_backward(A, A, W, act="relu", act_out=A, dx_add=A)):
+        assert _rel(f, n.double().cpu()) <= 2.0 ** -8
+
+
 @pytest.mark.parametrize("rows, k, n", [(50, 40, 24), (200, 41, 23), (200, 64, 64), (3000, 41, 123), (3000, 64, 128)])
 def test_fc_largest_values(rows, k, n):
     """fp32 values that no bf16 holds, with products that fp32 holds."""
